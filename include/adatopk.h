@@ -266,6 +266,82 @@ adatopk_status adatopk_plan_keep_counts(const double *alpha, const double *beta,
                                         adatopk_dtype dt, double r_user, double coeff, double *r_out,
                                         int64_t *k_out);
 
+/* ---- The training step of a pipeline stage around the link.  A stage keeps the activations of all micro-batches that are under way
+ * (n_b of them, Sec. 3.6) until their gradients come back over the slow link (backward pass of Sec. 3.3).  These calls keep them in 8 bits and
+ * run the backward pass from there.  Conventions as above; in addition:
+ *   - a dense matrix is `rows` rows of `cols` values, `stride` elements from one row to the next (stride >= cols; any stride and any alignment
+ *     to the element size; with one row the stride is not looked at).  Rows times columns, columns rounded up to 32, stay below 2^34;
+ *   - values are rounded to their type once, to nearest with ties to even; sums, statistics and the gradients of weights are fp32;
+ *   - weight and bias are of type weight_dt: that of the activations, or fp32;
+ *   - no output overlaps an input, but where it says so;
+ *   - rows == 0 or cols == 0 do nothing (gradients of weights over no rows are zero).
+ *
+ * An activation in 8 bits (`act8`): 32 consecutive elements of a row, the last group of a row being shorter, share a power of two as their
+ * scale (the layout that the OCP microscaling specification calls MXINT8).  With E = the exponent field, biased by 127 as in fp32, of
+ * the group's largest magnitude, but at least 7, an element x is held as
+ *     q = clamp(round_half_even(x / 2^(E - 133)), -127, 127)     and read back as     q * 2^(E - 133),
+ * so the error is at most 1 / 127.5 of the group's largest magnitude, and the result does not depend on the machine.  E = 255 marks a group with a NaN
+ * or an infinity; all of it reads back as NaN.  -0 is read back as +0.  The buffer: rows of numbers, each padded with zeros to a multiple of
+ * 32; from the next multiple of 256 bytes on one byte E per group, row by row.  16-byte aligned. */
+
+/* Host-only.  Bytes of the buffer of a rows x cols activation; 0 for invalid sizes. */
+size_t adatopk_act8_bytes(int64_t rows, int64_t cols);
+
+/* Puts a matrix away in 8 bits, and reads it back as type dt. */
+adatopk_status adatopk_act8_store(const void *x, int64_t x_stride, int64_t rows, int64_t cols, adatopk_dtype dt, void *act8, void *hip_stream);
+adatopk_status adatopk_act8_load(const void *act8, int64_t rows, int64_t cols, adatopk_dtype dt, void *y, int64_t y_stride, void *hip_stream);
+
+/* y = GELU(x): x * Phi(x), or with use_tanh != 0 the form x / 2 * (1 + tanh(sqrt(2 / pi) * (x + 0.044715 x^3))).
+ *   act8_x, act8_y   x and the rounded y put away in 8 bits, each NULL to skip: the first is what adatopk_gelu_backward reads, the second what
+ *                    adatopk_weight_grad of the next projection reads.  y may be x itself (same stride). */
+adatopk_status adatopk_gelu_forward(const void *x, int64_t x_stride, int64_t rows, int64_t cols, adatopk_dtype dt, int32_t use_tanh, void *y,
+                                    int64_t y_stride, void *act8_x, void *act8_y, void *hip_stream);
+
+/* dx = dy * GELU'(x), x as it reads back from act8_x.  dx may be dy itself (same stride). */
+adatopk_status adatopk_gelu_backward(const void *dy, int64_t dy_stride, const void *act8_x, int64_t rows, int64_t cols, adatopk_dtype dt,
+                                     int32_t use_tanh, void *dx, int64_t dx_stride, void *hip_stream);
+
+/* Layer norm of every row: s = x + residual, rounded to dt; mean = average of s; rstd = 1 / sqrt(average of (s - mean)^2 + eps);
+ * h = (s - mean) * rstd; y = weight * h + bias.  cols <= 32768.
+ *   residual     NULL: s = x
+ *   weight, bias NULL: ones, zeros
+ *   sum          s, or NULL to skip (only with a residual); may be x or residual itself (same stride)
+ *   mean, rstd   `rows` floats each, or NULL to skip
+ *   act8         h put away in 8 bits, or NULL to skip
+ * y may be x or residual itself (same stride) where no sum is written there. */
+adatopk_status adatopk_layernorm_forward(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight,
+                                         const void *bias, adatopk_dtype weight_dt, int64_t rows, int64_t cols, adatopk_dtype dt, float eps, void *sum,
+                                         int64_t sum_stride, void *y, int64_t y_stride, float *mean, float *rstd, void *act8, void *hip_stream);
+
+/* Backward pass of the layer norm.  With g = dy * weight and averages over the row,
+ *     dx = rstd * (g - average(g) - h * average(g * h)) + dsum,   dweight = sum over rows of dy * h,   dbias = sum over rows of dy.
+ *   x, act8      exactly one of the two: the normalised input s, from which h = (s - mean) * rstd, or h in 8 bits (mean is not read then)
+ *   dsum         gradient that reaches s on the residual path, or NULL
+ *   dx           may be dy or dsum itself (same stride)
+ *   dweight, dbias  `cols` floats each, or NULL to skip; accumulate != 0 adds to them (the micro-batches before)
+ *   workspace    device, 256-byte aligned, at least adatopk_layernorm_backward_workspace_bytes(rows, cols); not looked at where both are NULL
+ * The order of all sums is fixed: equal calls give equal bits. */
+size_t adatopk_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols);
+adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *act8, const float *mean,
+                                          const float *rstd, const void *weight, adatopk_dtype weight_dt, const void *dsum, int64_t dsum_stride,
+                                          int64_t rows, int64_t cols, adatopk_dtype dt, void *dx, int64_t dx_stride, float *dweight, float *dbias,
+                                          int32_t accumulate, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Gradient of a projection y = x W^T + b whose input was kept in 8 bits: dw = dy^T x (n_out rows of n_in floats, nothing between them),
+ * db = sum over rows of dy.  Products are exact, sums fp32 in a fixed order.
+ *   dy           rows x n_out, type dt
+ *   act8_x       the input, rows x n_in
+ *   weight, bias n_in values each, or NULL: the input was weight * h + bias with h what act8_x holds (a layer norm's normalised rows), and x is
+ *                that.  Either may be NULL alone (ones, zeros)
+ *   db           n_out floats, or NULL to skip
+ *   accumulate   != 0: added to dw and db
+ *   workspace    device, 256-byte aligned, at least adatopk_weight_grad_workspace_bytes(rows, n_out, n_in, dt)
+ * n_out, n_in <= 131072, rows < 2^31. */
+size_t adatopk_weight_grad_workspace_bytes(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt);
+adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void *act8_x, int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt,
+                                   const void *weight, const void *bias, adatopk_dtype weight_dt, float *dw, float *db, int32_t accumulate,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -140,6 +140,27 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.adatopk_plan_keep_counts.restype = i32
     lib.adatopk_compress_noalloc.argtypes = [p, i64, i32, i64, p, p, p, p]
     lib.adatopk_compress_noalloc.restype = i32
+    f32 = ctypes.c_float
+    lib.adatopk_act8_bytes.argtypes = [i64, i64]
+    lib.adatopk_act8_bytes.restype = sz
+    lib.adatopk_act8_store.argtypes = [p, i64, i64, i64, i32, p, p]
+    lib.adatopk_act8_store.restype = i32
+    lib.adatopk_act8_load.argtypes = [p, i64, i64, i32, p, i64, p]
+    lib.adatopk_act8_load.restype = i32
+    lib.adatopk_gelu_forward.argtypes = [p, i64, i64, i64, i32, i32, p, i64, p, p, p]
+    lib.adatopk_gelu_forward.restype = i32
+    lib.adatopk_gelu_backward.argtypes = [p, i64, p, i64, i64, i32, i32, p, i64, p]
+    lib.adatopk_gelu_backward.restype = i32
+    lib.adatopk_layernorm_forward.argtypes = [p, i64, p, i64, p, p, i32, i64, i64, i32, f32, p, i64, p, i64, p, p, p, p]
+    lib.adatopk_layernorm_forward.restype = i32
+    lib.adatopk_layernorm_backward_workspace_bytes.argtypes = [i64, i64]
+    lib.adatopk_layernorm_backward_workspace_bytes.restype = sz
+    lib.adatopk_layernorm_backward.argtypes = [p, i64, p, i64, p, p, p, p, i32, p, i64, i64, i64, i32, p, i64, p, p, i32, p, sz, p]
+    lib.adatopk_layernorm_backward.restype = i32
+    lib.adatopk_weight_grad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.adatopk_weight_grad_workspace_bytes.restype = sz
+    lib.adatopk_weight_grad.argtypes = [p, i64, p, i64, i64, i64, i32, p, p, i32, p, p, i32, p, sz, p]
+    lib.adatopk_weight_grad.restype = i32
     lib.address = _Addresses(lib)
     return lib
 
@@ -494,6 +515,150 @@ def adatopk_plan_keep_counts(alpha: Sequence[float], beta: Sequence[float], n: S
                                                    float(r_user), float(coeff), r_out, k_out),
            "adatopk_plan_keep_counts")
     return [r_out[i] for i in range(m)], [int(k_out[i]) for i in range(m)]
+
+
+# ------------------------------------------------------------------ the training step of a stage around the link
+# A matrix is a tensor whose last dimension is contiguous and whose other dimensions are rows at one distance from the next: contiguous tensors of any
+# number of dimensions, and views that cut columns out of one.
+def _matrix(t: torch.Tensor, what: str):
+    """(address, stride, rows, cols) of a tensor seen as rows of its last dimension."""
+    if not t.is_cuda:
+        raise ValueError("%s: adatopk needs device tensors" % what)
+    shape = t.shape
+    if not shape:
+        raise ValueError("%s needs at least one dimension" % what)
+    cols, strides = shape[-1], t.stride()
+    if cols > 1 and strides[-1] != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % what)
+    rows, stride = 1, cols
+    for size, step in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if size != 1:
+            if rows == 1:
+                stride = step
+            elif step != rows * stride:
+                raise ValueError("%s must have its rows at one distance from the next" % what)
+        rows *= size
+    return t.data_ptr(), stride, rows, cols
+
+
+def _like(t: Optional[torch.Tensor], dtype: torch.dtype, rows: int, cols: int, what: str):
+    """(address, stride) of another matrix of the call, (None, 0) for None."""
+    if t is None:
+        return None, 0
+    address, stride, r, c = _matrix(t, what)
+    if t.dtype != dtype or r != rows or c != cols:
+        raise ValueError("%s must be %s with %d rows of %d" % (what, dtype, rows, cols))
+    return address, stride
+
+
+def _floats(t: Optional[torch.Tensor], count: int, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != count:
+        raise ValueError("%s must be float32 with %d entries" % (what, count))
+    return _dev(t)
+
+
+def _act8(t: torch.Tensor, rows: int, cols: int, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.uint8 or t.numel() < adatopk_act8_bytes(rows, cols):
+        raise ValueError("%s must be uint8 with adatopk_act8_bytes(%d, %d) entries" % (what, rows, cols))
+    return _dev(t)
+
+
+def _weights(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], dtype: torch.dtype, cols: int):
+    """(address of the weight, of the bias, code of their type)."""
+    kind = weight.dtype if weight is not None else bias.dtype if bias is not None else dtype
+    for t, what in ((weight, "weight"), (bias, "bias")):
+        if t is not None and (t.dtype != kind or t.numel() != cols or kind not in (dtype, torch.float32)):
+            raise ValueError("%s must have %d entries of the activations' type or, like the other, of float32" % (what, cols))
+    return None if weight is None else _dev(weight), None if bias is None else _dev(bias), _dtype_code(kind)
+
+
+def adatopk_act8_bytes(rows: int, cols: int) -> int:
+    return int(load_library().adatopk_act8_bytes(int(rows), int(cols)))
+
+
+def new_act8(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    """Buffer of a rows x cols activation in 8 bits."""
+    return torch.empty(max(adatopk_act8_bytes(rows, cols), 16), dtype=torch.uint8, device=device)
+
+
+def adatopk_act8_store(x: torch.Tensor, act8: torch.Tensor) -> None:
+    """Puts a matrix away in 8 bits."""
+    address, stride, rows, cols = _matrix(x, "x")
+    _check(load_library().adatopk_act8_store(address, stride, rows, cols, _dtype_code(x.dtype), _act8(act8, rows, cols, "act8"), _stream()),
+           "adatopk_act8_store")
+
+
+def adatopk_act8_load(act8: torch.Tensor, y: torch.Tensor) -> None:
+    """Reads a matrix of y's shape back."""
+    address, stride, rows, cols = _matrix(y, "y")
+    _check(load_library().adatopk_act8_load(_act8(act8, rows, cols, "act8"), rows, cols, _dtype_code(y.dtype), address, stride, _stream()),
+           "adatopk_act8_load")
+
+
+def adatopk_gelu_forward(x: torch.Tensor, y: torch.Tensor, act8_x: Optional[torch.Tensor] = None, act8_y: Optional[torch.Tensor] = None,
+                         tanh: bool = False) -> None:
+    """y = GELU(x); x and y put away in 8 bits where buffers are given."""
+    address, stride, rows, cols = _matrix(x, "x")
+    _check(load_library().adatopk_gelu_forward(address, stride, rows, cols, _dtype_code(x.dtype), 1 if tanh else 0, *_like(y, x.dtype, rows, cols, "y"),
+                                               _act8(act8_x, rows, cols, "act8_x"), _act8(act8_y, rows, cols, "act8_y"), _stream()),
+           "adatopk_gelu_forward")
+
+
+def adatopk_gelu_backward(dy: torch.Tensor, act8_x: torch.Tensor, dx: torch.Tensor, tanh: bool = False) -> None:
+    """dx = dy * GELU'(x), x from its 8 bits."""
+    address, stride, rows, cols = _matrix(dy, "dy")
+    _check(load_library().adatopk_gelu_backward(address, stride, _act8(act8_x, rows, cols, "act8_x"), rows, cols, _dtype_code(dy.dtype), 1 if tanh else 0,
+                                                *_like(dx, dy.dtype, rows, cols, "dx"), _stream()), "adatopk_gelu_backward")
+
+
+def adatopk_layernorm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+                              mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor], residual: Optional[torch.Tensor] = None,
+                              sum_out: Optional[torch.Tensor] = None, act8: Optional[torch.Tensor] = None) -> None:
+    """y = layer norm of x + residual; the sum, the statistics and the normalised rows in 8 bits where buffers are given."""
+    address, stride, rows, cols = _matrix(x, "x")
+    _check(load_library().adatopk_layernorm_forward(
+        address, stride, *_like(residual, x.dtype, rows, cols, "residual"), *_weights(weight, bias, x.dtype, cols), rows, cols, _dtype_code(x.dtype),
+        float(eps), *_like(sum_out, x.dtype, rows, cols, "sum_out"), *_like(y, x.dtype, rows, cols, "y"), _floats(mean, rows, "mean"),
+        _floats(rstd, rows, "rstd"), _act8(act8, rows, cols, "act8"), _stream()), "adatopk_layernorm_forward")
+
+
+def adatopk_layernorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load_library().adatopk_layernorm_backward_workspace_bytes(int(rows), int(cols)))
+
+
+def adatopk_layernorm_backward(dy: torch.Tensor, x: Optional[torch.Tensor], act8: Optional[torch.Tensor], mean: Optional[torch.Tensor],
+                               rstd: torch.Tensor, weight: Optional[torch.Tensor], dx: torch.Tensor, dweight: Optional[torch.Tensor],
+                               dbias: Optional[torch.Tensor], workspace: Optional[torch.Tensor], dsum: Optional[torch.Tensor] = None,
+                               accumulate: bool = False) -> None:
+    """Gradients of a layer norm from its input x (with mean) or from its normalised rows in 8 bits; dsum is added to dx."""
+    address, stride, rows, cols = _matrix(dy, "dy")
+    weight_address, _, weight_code = _weights(weight, None, dy.dtype, cols)
+    _check(load_library().adatopk_layernorm_backward(
+        address, stride, *_like(x, dy.dtype, rows, cols, "x"), _act8(act8, rows, cols, "act8"), _floats(mean, rows, "mean"), _floats(rstd, rows, "rstd"),
+        weight_address, weight_code, *_like(dsum, dy.dtype, rows, cols, "dsum"), rows, cols, _dtype_code(dy.dtype), *_like(dx, dy.dtype, rows, cols, "dx"),
+        _floats(dweight, cols, "dweight"), _floats(dbias, cols, "dbias"), 1 if accumulate else 0, None if workspace is None else _dev(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()), "adatopk_layernorm_backward")
+
+
+def adatopk_weight_grad_workspace_bytes(rows: int, n_out: int, n_in: int, dtype: torch.dtype) -> int:
+    return int(load_library().adatopk_weight_grad_workspace_bytes(int(rows), int(n_out), int(n_in), _dtype_code(dtype)))
+
+
+def adatopk_weight_grad(dy: torch.Tensor, act8_x: torch.Tensor, dw: torch.Tensor, db: Optional[torch.Tensor], workspace: torch.Tensor,
+                        weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, accumulate: bool = False) -> None:
+    """dw = dy^T x and db, x from its 8 bits (behind a layer norm: weight * rows + bias)."""
+    address, stride, rows, n_out = _matrix(dy, "dy")
+    if dw.dim() != 2 or dw.dtype != torch.float32 or dw.shape[0] != n_out:
+        raise ValueError("dw must be float32 with %d rows, one for each of dy's columns" % n_out)
+    n_in = dw.shape[1]
+    _check(load_library().adatopk_weight_grad(
+        address, stride, _act8(act8_x, rows, n_in, "act8_x"), rows, n_out, n_in, _dtype_code(dy.dtype), *_weights(weight, bias, dy.dtype, n_in), _dev(dw),
+        _floats(db, n_out, "db"), 1 if accumulate else 0, _dev(workspace), workspace.numel() * workspace.element_size(), _stream()),
+        "adatopk_weight_grad")
 
 
 # ------------------------------------------------------------------ measurement hooks (measuring build only)

@@ -8,6 +8,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -18,10 +19,11 @@ MEASURE_LIB = os.path.join(HERE, "libadatopk_measure.so")
 MARSHAL_LIB = os.path.join(HERE, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
 HEADER = os.path.join(ROOT, "include", "adatopk.h")
-SOURCES = [os.path.join(CSRC, "adatopk.hip"), os.path.join(CSRC, "adatopk_host.cpp")]
+SOURCES = [os.path.join(CSRC, name) for name in ("adatopk.hip", "act8.hip", "layernorm.hip", "weight_grad.hip", "adatopk_host.cpp")]
+INTERNAL_HEADERS = [os.path.join(CSRC, name) for name in ("wire_layout.h", "act8_layout.h", "stage_ops.h")]
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
     # packed-fp32 instruction forms are kept out of the generated code on the test machines
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
@@ -29,12 +31,19 @@ HIPCC_FLAGS = [
 
 
 def build_library(verbose: bool = False, out: str = LIB, defines=()) -> str:
-    """Compiles the library to `out`; `defines` are extra -D macros (launch-shape overrides)."""
+    """Compiles the library to `out`, its sources side by side; `defines` are extra -D macros (launch-shape overrides)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + ["-D" + d for d in defines] + ["-o", out] + SOURCES
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    with tempfile.TemporaryDirectory() as scratch:
+        objects = [os.path.join(scratch, os.path.basename(source) + ".o") for source in SOURCES]
+        commands = [[hipcc] + HIPCC_FLAGS + ["-D" + d for d in defines] + ["-c", "-o", o, source] for o, source in zip(objects, SOURCES)]
+        link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", out] + objects
+        if verbose:
+            print("\n".join(" ".join(cmd) for cmd in commands + [link]), flush=True)
+        running = [subprocess.Popen(cmd) for cmd in commands]
+        failed = [cmd for cmd, code in [(p.args, p.wait()) for p in running] if code != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.run(link, check=True)
     return out
 
 
@@ -62,7 +71,7 @@ def library_is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = SOURCES + [HEADER, os.path.join(ROOT, "include", "adatopk_measure.h"), os.path.join(CSRC, "wire_layout.h")]
+    deps = SOURCES + [HEADER, os.path.join(ROOT, "include", "adatopk_measure.h")] + INTERNAL_HEADERS
     return any(os.path.getmtime(d) > t for d in deps)
 
 

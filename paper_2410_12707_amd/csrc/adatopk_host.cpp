@@ -6,6 +6,7 @@
 #include <cstdint>
 #include <cstring>
 
+#include "act8_layout.h"
 #include "adatopk.h"
 #include "wire_layout.h"
 
@@ -136,6 +137,12 @@ adatopk_status adatopk_wire_parse_header(const void *host_bytes, size_t wire_byt
         return ADATOPK_EINVAL;
     *out = h;
     return ADATOPK_OK;
+}
+
+size_t adatopk_act8_bytes(int64_t rows, int64_t cols) {
+    if (!adatopk_internal::act8_shape_ok(rows, cols)) return 0;
+    return adatopk_internal::act8_exponents_at(rows, cols) +
+           static_cast<size_t>(rows) * static_cast<size_t>(adatopk_internal::act8_pitch(cols) / adatopk_internal::ACT8_GROUP);
 }
 
 }  // extern "C"
