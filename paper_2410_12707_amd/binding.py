@@ -170,7 +170,8 @@ class _Addresses:
 
     def __init__(self, lib: ctypes.CDLL):
         for name in ("compress", "decompress", "decompress_sorted", "decompress_accumulate", "decompress_segmented", "compress_wire",
-                     "compress_wire_segmented", "decompress_wire", "compress_segmented"):
+                     "compress_wire_segmented", "decompress_wire", "compress_segmented", "act8_store", "act8_load", "gelu_forward", "gelu_backward",
+                     "layernorm_forward", "layernorm_backward", "weight_grad"):
             setattr(self, name, ctypes.cast(getattr(lib, "adatopk_" + name), ctypes.c_void_p).value)
 
 
@@ -233,7 +234,8 @@ def _check_pairs(dtype: torch.dtype, k_total: int, idx: torch.Tensor, val: torch
 
 _marshal = None  # the extension that reads the arguments and makes the calls; False: there is none
 _MARSHAL_NAMES = ("tensors", "int64s", "streams", "compress", "decompress", "compress_wire", "decompress_wire", "compress_segmented",
-                  "decompress_segmented", "compress_wire_segmented")
+                  "decompress_segmented", "compress_wire_segmented", "act8_store", "act8_load", "gelu_forward", "gelu_backward", "layernorm_forward",
+                  "layernorm_backward", "weight_grad")
 
 
 def _load_marshal():
@@ -587,31 +589,47 @@ def new_act8(rows: int, cols: int, device="cuda") -> torch.Tensor:
 
 def adatopk_act8_store(x: torch.Tensor, act8: torch.Tensor) -> None:
     """Puts a matrix away in 8 bits."""
+    lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.act8_store(lib.address.act8_store, x, act8), "adatopk_act8_store"):
+        return
     address, stride, rows, cols = _matrix(x, "x")
-    _check(load_library().adatopk_act8_store(address, stride, rows, cols, _dtype_code(x.dtype), _act8(act8, rows, cols, "act8"), _stream()),
+    _check(lib.adatopk_act8_store(address, stride, rows, cols, _dtype_code(x.dtype), _act8(act8, rows, cols, "act8"), _stream()),
            "adatopk_act8_store")
 
 
 def adatopk_act8_load(act8: torch.Tensor, y: torch.Tensor) -> None:
     """Reads a matrix of y's shape back."""
+    lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.act8_load(lib.address.act8_load, act8, y), "adatopk_act8_load"):
+        return
     address, stride, rows, cols = _matrix(y, "y")
-    _check(load_library().adatopk_act8_load(_act8(act8, rows, cols, "act8"), rows, cols, _dtype_code(y.dtype), address, stride, _stream()),
+    _check(lib.adatopk_act8_load(_act8(act8, rows, cols, "act8"), rows, cols, _dtype_code(y.dtype), address, stride, _stream()),
            "adatopk_act8_load")
 
 
 def adatopk_gelu_forward(x: torch.Tensor, y: torch.Tensor, act8_x: Optional[torch.Tensor] = None, act8_y: Optional[torch.Tensor] = None,
                          tanh: bool = False) -> None:
     """y = GELU(x); x and y put away in 8 bits where buffers are given."""
+    lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.gelu_forward(lib.address.gelu_forward, x, y, act8_x, act8_y, tanh), "adatopk_gelu_forward"):
+        return
     address, stride, rows, cols = _matrix(x, "x")
-    _check(load_library().adatopk_gelu_forward(address, stride, rows, cols, _dtype_code(x.dtype), 1 if tanh else 0, *_like(y, x.dtype, rows, cols, "y"),
+    _check(lib.adatopk_gelu_forward(address, stride, rows, cols, _dtype_code(x.dtype), 1 if tanh else 0, *_like(y, x.dtype, rows, cols, "y"),
                                                _act8(act8_x, rows, cols, "act8_x"), _act8(act8_y, rows, cols, "act8_y"), _stream()),
            "adatopk_gelu_forward")
 
 
 def adatopk_gelu_backward(dy: torch.Tensor, act8_x: torch.Tensor, dx: torch.Tensor, tanh: bool = False) -> None:
     """dx = dy * GELU'(x), x from its 8 bits."""
+    lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.gelu_backward(lib.address.gelu_backward, dy, act8_x, dx, tanh), "adatopk_gelu_backward"):
+        return
     address, stride, rows, cols = _matrix(dy, "dy")
-    _check(load_library().adatopk_gelu_backward(address, stride, _act8(act8_x, rows, cols, "act8_x"), rows, cols, _dtype_code(dy.dtype), 1 if tanh else 0,
+    _check(lib.adatopk_gelu_backward(address, stride, _act8(act8_x, rows, cols, "act8_x"), rows, cols, _dtype_code(dy.dtype), 1 if tanh else 0,
                                                 *_like(dx, dy.dtype, rows, cols, "dx"), _stream()), "adatopk_gelu_backward")
 
 
@@ -619,8 +637,12 @@ def adatopk_layernorm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], b
                               mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor], residual: Optional[torch.Tensor] = None,
                               sum_out: Optional[torch.Tensor] = None, act8: Optional[torch.Tensor] = None) -> None:
     """y = layer norm of x + residual; the sum, the statistics and the normalised rows in 8 bits where buffers are given."""
+    lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.layernorm_forward(lib.address.layernorm_forward, x, weight, bias, eps, y, mean, rstd, residual, sum_out, act8), "adatopk_layernorm_forward"):
+        return
     address, stride, rows, cols = _matrix(x, "x")
-    _check(load_library().adatopk_layernorm_forward(
+    _check(lib.adatopk_layernorm_forward(
         address, stride, *_like(residual, x.dtype, rows, cols, "residual"), *_weights(weight, bias, x.dtype, cols), rows, cols, _dtype_code(x.dtype),
         float(eps), *_like(sum_out, x.dtype, rows, cols, "sum_out"), *_like(y, x.dtype, rows, cols, "y"), _floats(mean, rows, "mean"),
         _floats(rstd, rows, "rstd"), _act8(act8, rows, cols, "act8"), _stream()), "adatopk_layernorm_forward")
@@ -635,9 +657,13 @@ def adatopk_layernorm_backward(dy: torch.Tensor, x: Optional[torch.Tensor], act8
                                dbias: Optional[torch.Tensor], workspace: Optional[torch.Tensor], dsum: Optional[torch.Tensor] = None,
                                accumulate: bool = False) -> None:
     """Gradients of a layer norm from its input x (with mean) or from its normalised rows in 8 bits; dsum is added to dx."""
+    lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.layernorm_backward(lib.address.layernorm_backward, dy, x, act8, mean, rstd, weight, dx, dweight, dbias, workspace, dsum, accumulate), "adatopk_layernorm_backward"):
+        return
     address, stride, rows, cols = _matrix(dy, "dy")
     weight_address, _, weight_code = _weights(weight, None, dy.dtype, cols)
-    _check(load_library().adatopk_layernorm_backward(
+    _check(lib.adatopk_layernorm_backward(
         address, stride, *_like(x, dy.dtype, rows, cols, "x"), _act8(act8, rows, cols, "act8"), _floats(mean, rows, "mean"), _floats(rstd, rows, "rstd"),
         weight_address, weight_code, *_like(dsum, dy.dtype, rows, cols, "dsum"), rows, cols, _dtype_code(dy.dtype), *_like(dx, dy.dtype, rows, cols, "dx"),
         _floats(dweight, cols, "dweight"), _floats(dbias, cols, "dbias"), 1 if accumulate else 0, None if workspace is None else _dev(workspace),
@@ -651,11 +677,15 @@ def adatopk_weight_grad_workspace_bytes(rows: int, n_out: int, n_in: int, dtype:
 def adatopk_weight_grad(dy: torch.Tensor, act8_x: torch.Tensor, dw: torch.Tensor, db: Optional[torch.Tensor], workspace: torch.Tensor,
                         weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, accumulate: bool = False) -> None:
     """dw = dy^T x and db, x from its 8 bits (behind a layer norm: weight * rows + bias)."""
+    lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.weight_grad(lib.address.weight_grad, dy, act8_x, dw, db, workspace, weight, bias, accumulate), "adatopk_weight_grad"):
+        return
     address, stride, rows, n_out = _matrix(dy, "dy")
     if dw.dim() != 2 or dw.dtype != torch.float32 or dw.shape[0] != n_out:
         raise ValueError("dw must be float32 with %d rows, one for each of dy's columns" % n_out)
     n_in = dw.shape[1]
-    _check(load_library().adatopk_weight_grad(
+    _check(lib.adatopk_weight_grad(
         address, stride, _act8(act8_x, rows, n_in, "act8_x"), rows, n_out, n_in, _dtype_code(dy.dtype), *_weights(weight, bias, dy.dtype, n_in), _dev(dw),
         _floats(db, n_out, "db"), 1 if accumulate else 0, _dev(workspace), workspace.numel() * workspace.element_size(), _stream()),
         "adatopk_weight_grad")

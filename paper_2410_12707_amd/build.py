@@ -59,7 +59,7 @@ def build_marshal(verbose: bool = False) -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
            "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
-           "-isystem", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"), "-Wall", "-Wextra", "-o", MARSHAL_LIB, MARSHAL_SOURCE,
+           "-isystem", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wall", "-Wextra", "-o", MARSHAL_LIB, MARSHAL_SOURCE,
            "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
     if verbose:
         print(" ".join(cmd), flush=True)

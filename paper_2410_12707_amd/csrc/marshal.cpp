@@ -17,6 +17,7 @@
 
 #include <vector>
 
+#include "act8_layout.h"
 #include "adatopk.h"
 
 namespace {
@@ -200,6 +201,83 @@ struct Call {
     }
 };
 
+// A tensor seen as rows of its last dimension, which is contiguous: its other dimensions are rows at one distance from the next.
+struct Matrix {
+    void *data = nullptr;
+    int64_t stride = 0, rows = 0, cols = 0;
+    at::ScalarType type = at::ScalarType::Undefined;
+
+    Matrix(Call &c, PyObject *o) {
+        if (!c.plain || !THPVariable_CheckExact(o)) {
+            c.plain = false;
+            return;
+        }
+        const at::Tensor &t = THPVariable_Unpack(o);
+        const int64_t dims = t.dim();
+        c.plain = t.is_cuda() && t.layout() == at::kStrided && dims >= 1;
+        if (!c.plain) return;
+        type = t.scalar_type();
+        cols = t.size(dims - 1);
+        c.plain = cols <= 1 || t.stride(dims - 1) == 1;
+        rows = 1;
+        stride = cols;
+        for (int64_t d = dims - 2; d >= 0 && c.plain; --d) {
+            const int64_t size = t.size(d), step = t.stride(d);
+            if (size != 1) {
+                if (rows == 1)
+                    stride = step;
+                else
+                    c.plain = step == rows * stride;
+            }
+            rows *= size;
+        }
+        data = c.address(&t);
+    }
+    // Another matrix of the call, of the same type and shape, or nothing.
+    Matrix(Call &c, PyObject *o, const Matrix &like) {
+        if (o == Py_None) return;
+        *this = Matrix(c, o);
+        c.plain = c.plain && type == like.type && rows == like.rows && cols == like.cols;
+    }
+};
+float *floats(Call &c, PyObject *o, int64_t count) {  // exactly so many, or nothing
+    if (o == Py_None) return nullptr;
+    const at::Tensor *t = c.tensor(o);
+    if (t != nullptr) c.plain = t->scalar_type() == at::ScalarType::Float && t->numel() == count;
+    return static_cast<float *>(c.address(t));
+}
+void *act8(Call &c, PyObject *o, int64_t rows, int64_t cols) {
+    if (o == Py_None) return nullptr;
+    if (!adatopk_internal::act8_shape_ok(rows, cols)) c.plain = false;
+    return c.buffer(o, at::ScalarType::Byte,
+                    c.plain ? static_cast<int64_t>(adatopk_internal::act8_exponents_at(rows, cols)) + rows * (adatopk_internal::act8_pitch(cols) / adatopk_internal::ACT8_GROUP)
+                            : 0);
+}
+struct Weights {
+    const void *weight = nullptr, *bias = nullptr;
+    adatopk_dtype type = ADATOPK_F32;
+    Weights(Call &c, PyObject *w, PyObject *b, at::ScalarType kind, int64_t cols) {
+        const at::Tensor *tw = w != Py_None ? c.tensor(w) : nullptr, *tb = b != Py_None ? c.tensor(b) : nullptr;
+        const at::ScalarType own = tw != nullptr ? tw->scalar_type() : (tb != nullptr ? tb->scalar_type() : kind);
+        c.plain = c.plain && (own == kind || own == at::ScalarType::Float) && (tw == nullptr || tw->numel() == cols) &&
+                  (tb == nullptr || (tb->numel() == cols && tb->scalar_type() == own));
+        if (!c.plain) return;
+        weight = c.address(tw);
+        bias = c.address(tb);
+        type = c.dtype(own);
+    }
+};
+struct Workspace {
+    void *data = nullptr;
+    size_t bytes = 0;
+    Workspace(Call &c, PyObject *o) {
+        if (o == Py_None) return;
+        const at::Tensor *t = c.tensor(o);
+        data = c.address(t);
+        if (c.plain) bytes = t->nbytes();
+    }
+};
+
 // The body of a call: `f` reads the arguments and returns the status; what it throws (a wrapper of functorch, a tensor without storage)
 // and what is not plain is left to Python.  An exception out of Python code, that of a signal among them (an interrupt while the stream is asked for),
 // is the call's: nothing has been enqueued.
@@ -365,6 +443,107 @@ PyObject *compress_wire_segmented(PyObject *, PyObject *const *a, Py_ssize_t nar
     });
 }
 
+// (fn, x, act8)
+PyObject *act8_store(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 3, [&](Call &c) -> long {
+        const Matrix x(c, a[1]);
+        const adatopk_dtype dt = c.dtype(x.type);
+        void *q = a[2] != Py_None ? act8(c, a[2], x.rows, x.cols) : nullptr, *stream = c.stream();
+        return without_gil<decltype(&adatopk_act8_store)>(c, a[0], static_cast<const void *>(x.data), x.stride, x.rows, x.cols, dt, q, stream);
+    });
+}
+
+// (fn, act8, y)
+PyObject *act8_load(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 3, [&](Call &c) -> long {
+        const Matrix y(c, a[2]);
+        const adatopk_dtype dt = c.dtype(y.type);
+        void *q = act8(c, a[1], y.rows, y.cols), *stream = c.stream();
+        return without_gil<decltype(&adatopk_act8_load)>(c, a[0], static_cast<const void *>(q), y.rows, y.cols, dt, y.data, y.stride, stream);
+    });
+}
+
+// (fn, x, y, act8_x or None, act8_y or None, tanh)
+PyObject *gelu_forward(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 6, [&](Call &c) -> long {
+        const Matrix x(c, a[1]), y(c, a[2], x);
+        const adatopk_dtype dt = c.dtype(x.type);
+        void *qx = act8(c, a[3], x.rows, x.cols), *qy = act8(c, a[4], x.rows, x.cols);
+        const int tanh = c.truth(a[5]);
+        void *stream = c.stream();
+        return without_gil<decltype(&adatopk_gelu_forward)>(c, a[0], static_cast<const void *>(x.data), x.stride, x.rows, x.cols, dt, tanh, y.data, y.stride, qx, qy,
+                                                            stream);
+    });
+}
+
+// (fn, dy, act8, dx, tanh)
+PyObject *gelu_backward(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 5, [&](Call &c) -> long {
+        const Matrix dy(c, a[1]), dx(c, a[3], dy);
+        const adatopk_dtype dt = c.dtype(dy.type);
+        void *q = act8(c, a[2], dy.rows, dy.cols);
+        const int tanh = c.truth(a[4]);
+        void *stream = c.stream();
+        return without_gil<decltype(&adatopk_gelu_backward)>(c, a[0], static_cast<const void *>(dy.data), dy.stride, static_cast<const void *>(q), dy.rows, dy.cols,
+                                                             dt, tanh, dx.data, dx.stride, stream);
+    });
+}
+
+// (fn, x, weight or None, bias or None, eps, y, mean or None, rstd or None, residual or None, sum or None, act8 or None)
+PyObject *layernorm_forward(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 11, [&](Call &c) -> long {
+        const Matrix x(c, a[1]), y(c, a[5], x), residual(c, a[8], x), sum(c, a[9], x);
+        const adatopk_dtype dt = c.dtype(x.type);
+        const Weights w(c, a[2], a[3], x.type, x.cols);
+        c.plain = c.plain && PyFloat_CheckExact(a[4]);
+        float *mean = floats(c, a[6], x.rows), *rstd = floats(c, a[7], x.rows);
+        void *q = act8(c, a[10], x.rows, x.cols), *stream = c.stream();
+        if (!c.plain) return 0;
+        return without_gil<decltype(&adatopk_layernorm_forward)>(
+            c, a[0], static_cast<const void *>(x.data), x.stride, static_cast<const void *>(residual.data), residual.stride, w.weight, w.bias, w.type, x.rows, x.cols,
+            dt, static_cast<float>(PyFloat_AS_DOUBLE(a[4])), sum.data, sum.stride, y.data, y.stride, mean, rstd, q, stream);
+    });
+}
+
+// (fn, dy, x or None, act8 or None, mean or None, rstd, weight or None, dx, dweight or None, dbias or None, workspace or None, dsum or None, accumulate)
+PyObject *layernorm_backward(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 13, [&](Call &c) -> long {
+        const Matrix dy(c, a[1]), x(c, a[2], dy), dx(c, a[7], dy), dsum(c, a[11], dy);
+        const adatopk_dtype dt = c.dtype(dy.type);
+        const Weights w(c, a[6], Py_None, dy.type, dy.cols);
+        void *q = act8(c, a[3], dy.rows, dy.cols);
+        float *mean = floats(c, a[4], dy.rows), *rstd = floats(c, a[5], dy.rows), *dw = floats(c, a[8], dy.cols), *db = floats(c, a[9], dy.cols);
+        const Workspace ws(c, a[10]);
+        const int accumulate = c.truth(a[12]);
+        void *stream = c.stream();
+        return without_gil<decltype(&adatopk_layernorm_backward)>(
+            c, a[0], static_cast<const void *>(dy.data), dy.stride, static_cast<const void *>(x.data), x.stride, static_cast<const void *>(q),
+            static_cast<const float *>(mean), static_cast<const float *>(rstd), w.weight, w.type, static_cast<const void *>(dsum.data), dsum.stride, dy.rows, dy.cols,
+            dt, dx.data, dx.stride, dw, db, accumulate, ws.data, ws.bytes, stream);
+    });
+}
+
+// (fn, dy, act8, dw, db or None, workspace, weight or None, bias or None, accumulate)
+PyObject *weight_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 9, [&](Call &c) -> long {
+        const Matrix dy(c, a[1]);
+        const adatopk_dtype dt = c.dtype(dy.type);
+        const at::Tensor *dw = c.tensor(a[3]);
+        c.plain = c.plain && dw->dim() == 2 && dw->scalar_type() == at::ScalarType::Float && dw->size(0) == dy.cols;
+        if (!c.plain) return 0;
+        const int64_t n_in = dw->size(1);
+        void *q = a[2] != Py_None ? act8(c, a[2], dy.rows, n_in) : nullptr;
+        const Weights w(c, a[6], a[7], dy.type, n_in);
+        float *db = floats(c, a[4], dy.cols);
+        const Workspace ws(c, a[5]);
+        const int accumulate = c.truth(a[8]);
+        void *stream = c.stream();
+        return without_gil<decltype(&adatopk_weight_grad)>(c, a[0], static_cast<const void *>(dy.data), dy.stride, static_cast<const void *>(q), dy.rows, dy.cols, n_in,
+                                                           dt, w.weight, w.bias, w.type, static_cast<float *>(c.address(dw)), db, accumulate, ws.data, ws.bytes,
+                                                           stream);
+    });
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)> constexpr PyMethodDef fast(const char *name, const char *doc) {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(F)), METH_FASTCALL, doc};
 }
@@ -379,6 +558,13 @@ PyMethodDef methods[] = {
     fast<compress_segmented>("compress_segmented", "status of the call at an address, or None"),
     fast<decompress_segmented>("decompress_segmented", "status of the call at an address, or None"),
     fast<compress_wire_segmented>("compress_wire_segmented", "status of the call at an address, or None"),
+    fast<act8_store>("act8_store", "status of the call at an address, or None"),
+    fast<act8_load>("act8_load", "status of the call at an address, or None"),
+    fast<gelu_forward>("gelu_forward", "status of the call at an address, or None"),
+    fast<gelu_backward>("gelu_backward", "status of the call at an address, or None"),
+    fast<layernorm_forward>("layernorm_forward", "status of the call at an address, or None"),
+    fast<layernorm_backward>("layernorm_backward", "status of the call at an address, or None"),
+    fast<weight_grad>("weight_grad", "status of the call at an address, or None"),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "The calls of the library, their arguments read in C.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
