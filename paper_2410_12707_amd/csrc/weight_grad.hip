@@ -27,7 +27,6 @@ template <typename T> constexpr int pieces_of() { return sizeof(T) == 4 ? 3 : (_
 typedef __bf16 Pair __attribute__((ext_vector_type(2)));
 
 constexpr int PAD = 32;  // elements behind a row of a tile in LDS: the four rows that one transposing read takes lie in different banks
-constexpr int WM = 2, WN = 2, NT = WM * WN * 64;  // wavefronts along the tile's two sides
 
 struct Product {
     const void *dy;
@@ -44,9 +43,10 @@ struct Product {
 };
 
 // The leading piece of each of two floats (bits cut off, so what is left is exact), and what is left.
-__device__ __forceinline__ uint32_t cut(float &lo, float &hi) {
+__device__ __forceinline__ uint32_t cut(float &lo, float &hi, bool first) {
     const uint32_t a = __float_as_uint(lo) & 0xFFFF0000u, b = __float_as_uint(hi) & 0xFFFF0000u;
-    const bool inf_a = __builtin_fabsf(lo) == __builtin_inff(), inf_b = __builtin_fabsf(hi) == __builtin_inff();
+    // (of an infinity nothing is left, and nothing of what is left is one; of a NaN, a NaN)
+    const bool inf_a = first && __builtin_fabsf(lo) == __builtin_inff(), inf_b = first && __builtin_fabsf(hi) == __builtin_inff();
     lo = inf_a ? 0.f : lo - __uint_as_float(a);
     hi = inf_b ? 0.f : hi - __uint_as_float(b);
     return a >> 16 | b;
@@ -71,12 +71,14 @@ __device__ __forceinline__ int place(int b, int n) {
 //
 // The last tile of a row or column of tiles begins so far ahead that it ends with the matrix (it stores what is its own), so loads need no bounds but
 // those of the tokens.  SMALL: the matrix is narrower than the tile, or its rows too far apart for 32-bit offsets; every load is bounded.
-template <typename T, int BM, int BN, int BK, bool SMALL> __global__ __launch_bounds__(NT, 1) void k_weight_grad(Product f) {
+template <typename T, int BM, int BN, int BK, int WM, int WN, int PER_CU, int AHEAD, bool SMALL>
+__global__ __launch_bounds__(WM *WN * 64, PER_CU * WM * WN / 4) void k_weight_grad(Product f) {
+    constexpr int NT = WM * WN * 64;
     constexpr int P = pieces_of<T>(), MI = BM / WM / 32, NI = BN / WN / 32, STEPS = BK / 16;
     constexpr int A_PITCH = BM + PAD, B_PITCH = BN + PAD, A_SIZE = BK * A_PITCH, BUFFER = P * A_SIZE + BK * B_PITCH;
-    constexpr int A_OCTETS = BK * BM / 8 / NT, B_ALL = BK * BN / 16, B_PIECES = (B_ALL + NT - 1) / NT;
-    static_assert(BK * BM % (8 * NT) == 0 && MI >= 1 && NI >= 1, "whole octets");
-    static_assert(NT % (BM / 8) == 0 && NT % 4 == 0, "an octet's column is the same in all of a thread's tokens");
+    constexpr int A_OCTETS = BK * BM / 8 / NT, BW = BK * BN / 16 % NT == 0 ? 16 : 8, B_PIECES = BK * BN / BW / NT;
+    constexpr int A_ROWS = NT / (BM / 8), B_ROWS = NT / (BN / BW);  // tokens from one of a thread's pieces of a tile to the next
+    static_assert(BK * BM % (8 * NT) == 0 && BK * BN % (BW * NT) == 0 && NT % (BM / 8) == 0 && MI >= 1 && NI >= 1, "whole pieces");
     __shared__ __attribute__((aligned(16))) uint16_t lds[2 * BUFFER];
     __shared__ float sums[BM];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, wm = wave / WN, wn = wave % WN;
@@ -86,88 +88,111 @@ template <typename T, int BM, int BN, int BK, bool SMALL> __global__ __launch_bo
     const int64_t out0 = SMALL || own_out + BM <= f.n_out ? own_out : f.n_out - BM, in0 = SMALL || own_in + BN <= f.x.pitch ? own_in : f.x.pitch - BN;
     const int64_t row0 = part * f.rows_per_split, row_end = row0 + f.rows_per_split < f.rows ? row0 + f.rows_per_split : f.rows;
 
-    Raw<T> ra[A_OCTETS];
-    U4 rb[B_PIECES];
-    uint32_t re[B_PIECES];
+    Raw<T> ra[AHEAD][A_OCTETS];  // of the AHEAD tiles behind the one in the next buffer
+    typedef uint32_t Numbers __attribute__((ext_vector_type(BW / 4)));
+    Numbers rb[AHEAD][B_PIECES];
+    uint32_t re[AHEAD][B_PIECES];
+    const int a_row = tid / (BM / 8), a_col = tid % (BM / 8) * 8;
     const uint32_t e_pitch = static_cast<uint32_t>(f.x.pitch / GROUP);
-    uint32_t a_at[A_OCTETS], b_at[B_PIECES], e_at[B_PIECES];  // bytes from a tile's first element
+    const uint32_t a_at = (static_cast<uint32_t>(a_row) * static_cast<uint32_t>(f.dy_stride) + a_col) * sizeof(T);  // bytes from a tile's first element
+    // (BN / BW need not divide NT: then a thread's pieces lie in different columns)
+    constexpr bool B_EVEN = NT % (BN / BW) == 0;
+    auto b_row = [&](int i) { return B_EVEN ? tid / (BN / BW) + i * B_ROWS : (tid + i * NT) / (BN / BW); };
+    auto b_col = [&](int i) { return (B_EVEN ? tid : tid + i * NT) % (BN / BW) * BW; };
+    uint32_t b_at[B_EVEN ? 1 : B_PIECES], e_at[B_EVEN ? 1 : B_PIECES];
 #pragma unroll
-    for (int i = 0; i < A_OCTETS; ++i) {
-        const int at = tid + i * NT;
-        a_at[i] = (static_cast<uint32_t>(at / (BM / 8)) * static_cast<uint32_t>(f.dy_stride) + at % (BM / 8) * 8) * sizeof(T);
+    for (int i = 0; i < (B_EVEN ? 1 : B_PIECES); ++i) {
+        b_at[i] = static_cast<uint32_t>(b_row(i)) * static_cast<uint32_t>(f.x.pitch) + b_col(i);
+        e_at[i] = b_row(i) * e_pitch + b_col(i) / GROUP;
     }
-#pragma unroll
-    for (int i = 0; i < B_PIECES; ++i) {
-        const uint32_t at = B_ALL % NT != 0 && tid + i * NT >= B_ALL ? 0 : tid + i * NT;
-        b_at[i] = at / (BN / 16) * static_cast<uint32_t>(f.x.pitch) + at % (BN / 16) * 16;
-        e_at[i] = at / (BN / 16) * e_pitch + at % (BN / 16) / 2;
-    }
-    auto fetch = [&](int64_t row) {
-        if (!SMALL && row + BK <= row_end) {
-            const char *const a = reinterpret_cast<const char *>(static_cast<const T *>(f.dy) + row * f.dy_stride + out0);
-            const char *const q = reinterpret_cast<const char *>(f.x.q + row * f.x.pitch + in0);
-            const uint8_t *const e = f.x.e + row * e_pitch + in0 / GROUP;
+    // Part `which` of `parts` of the tile that begins with token `row`, into registers.  WITHIN: all of its tokens are there.
+    auto fetch = [&](auto within, int set, int64_t row, int which, int parts) {
+        constexpr bool WITHIN = decltype(within)::value;
+        typedef const __attribute__((address_space(1))) char Global;
+        if constexpr (WITHIN) {
+            // (scalar bases that the optimiser cannot see through: an address is a base and a 32-bit offset, not a 64-bit variable of its own)
 #pragma unroll
             for (int i = 0; i < B_PIECES; ++i) {
-                rb[i] = *reinterpret_cast<const U4 *>(q + b_at[i]);
-                re[i] = e[e_at[i]];
+                if (i % parts != which) continue;
+                const int64_t r = row + (B_EVEN ? i * B_ROWS : 0);
+                uint64_t q = reinterpret_cast<uint64_t>(f.x.q + r * f.x.pitch + in0), e = reinterpret_cast<uint64_t>(f.x.e + r * e_pitch + in0 / GROUP);
+                asm("" : "+s"(q), "+s"(e));
+                rb[set][i] = *(const __attribute__((address_space(1))) Numbers *)((Global *)q + b_at[B_EVEN ? 0 : i]);
+                re[set][i] = *(const __attribute__((address_space(1))) uint8_t *)((Global *)e + e_at[B_EVEN ? 0 : i]);
             }
 #pragma unroll
-            for (int i = 0; i < A_OCTETS; ++i) ra[i] = load_octet(reinterpret_cast<const T *>(a + a_at[i]));
-            return;
-        }
+            for (int i = 0; i < A_OCTETS; ++i) {
+                if (i % parts != which) continue;
+                uint64_t a = reinterpret_cast<uint64_t>(static_cast<const T *>(f.dy) + (row + i * A_ROWS) * f.dy_stride + out0);
+                asm("" : "+s"(a));
+                const auto at = (Global *)a + a_at;
+                if constexpr (sizeof(T) == 4) {
+                    ra[set][i].w[0] = *(const __attribute__((address_space(1))) U4a4 *)at;
+                    ra[set][i].w[1] = *(const __attribute__((address_space(1))) U4a4 *)(at + 16);
+                } else {
+                    ra[set][i].w[0] = *(const __attribute__((address_space(1))) U4a2 *)at;
+                }
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < A_OCTETS; ++i) {
-            const int at = tid + i * NT;
-            const int64_t r = row + at / (BM / 8), c = out0 + at % (BM / 8) * 8;
-            ra[i] = load_row(static_cast<const T *>(f.dy) + r * f.dy_stride + c, r < row_end ? f.n_out - c : 0);
-        }
+            for (int i = 0; i < B_PIECES; ++i) {
+                if (i % parts != which) continue;
+                const int64_t r = row + b_row(i), c = in0 + b_col(i);
+                const bool there = r < row_end && c < f.x.pitch;
+                rb[set][i] = there ? *reinterpret_cast<const Numbers *>(f.x.q + r * f.x.pitch + c) : Numbers{};
+                re[set][i] = there ? f.x.e[r * (f.x.pitch / GROUP) + c / GROUP] : 7;
+            }
 #pragma unroll
-        for (int i = 0; i < B_PIECES; ++i) {
-            const int at = tid + i * NT;
-            const int64_t r = row + at / (BN / 16), c = in0 + at % (BN / 16) * 16;
-            const bool there = r < row_end && c < f.x.pitch && (B_ALL % NT == 0 || at < B_ALL);
-            rb[i] = there ? *reinterpret_cast<const U4 *>(f.x.q + r * f.x.pitch + c) : U4{0, 0, 0, 0};
-            re[i] = there ? f.x.e[r * (f.x.pitch / GROUP) + c / GROUP] : 7;
+            for (int i = 0; i < A_OCTETS; ++i) {
+                if (i % parts != which) continue;
+                const int64_t r = row + a_row + i * A_ROWS, c = out0 + a_col;
+                ra[set][i] = load_row(static_cast<const T *>(f.dy) + r * f.dy_stride + c, r < row_end ? f.n_out - c : 0);
+            }
         }
     };
     // Part `which` of `parts` of the tile in registers, into a buffer.
-    auto stage = [&](uint16_t *to, int which, int parts) {
+    auto stage = [&](int set, uint16_t *to, int which, int parts) {
+        uint16_t *const a = to + a_row * A_PITCH + a_col, *const x = to + P * A_SIZE;
 #pragma unroll
         for (int i = 0; i < A_OCTETS; ++i) {
             if (i % parts != which) continue;
-            const int at = tid + i * NT, k = at / (BM / 8), m = at % (BM / 8) * 8;
             if constexpr (P == 1) {
-                *reinterpret_cast<U4 *>(to + k * A_PITCH + m) = ra[i].w[0];
+                *reinterpret_cast<U4 *>(a + i * A_ROWS * A_PITCH) = ra[set][i].w[0];
             } else {
                 float v[8];
-                unpack(ra[i], v);
+                unpack(ra[set][i], v);
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
                     U4 d;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) d[j] = cut(v[2 * j], v[2 * j + 1]);
-                    *reinterpret_cast<U4 *>(to + p * A_SIZE + k * A_PITCH + m) = d;
+                    for (int j = 0; j < 4; ++j) d[j] = cut(v[2 * j], v[2 * j + 1], p == 0);
+                    *reinterpret_cast<U4 *>(a + p * A_SIZE + i * A_ROWS * A_PITCH) = d;
                 }
             }
         }
 #pragma unroll
         for (int i = 0; i < B_PIECES; ++i) {
             if (i % parts != which) continue;
-            const int at = tid + i * NT, k = at / (BN / 16), n = at % (BN / 16) * 16;
-            if (B_ALL % NT != 0 && at >= B_ALL) continue;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < BW / 8; ++h) {
                 float v[8];
-                values_of(U2{rb[i][2 * h], rb[i][2 * h + 1]}, re[i], v);
-                *reinterpret_cast<U4 *>(to + P * A_SIZE + k * B_PITCH + n + 8 * h) = pack<Bf16>(v).w[0];
+                values_of(U2{rb[set][i][2 * h], rb[set][i][2 * h + 1]}, re[set][i], v);
+                *reinterpret_cast<U4 *>(x + b_row(i) * B_PITCH + b_col(i) + 8 * h) = pack<Bf16>(v).w[0];
             }
         }
     };
     // What a lane holds of a 32 x 16 operand: feature lane % 32, tokens 8 * (lane / 32) and the seven behind it.  A transposing read works on blocks of
     // 16 lanes: lane i reads four features of token i / 4, and gets four tokens of feature i.
+    //
+    // The WN wavefronts along the tile's second side hold the same blocks of dY, each in an order that puts first the blocks whose sums over the tokens
+    // it takes: block(i).
+    constexpr int CI = (MI + WN - 1) / WN, TURN = MI < WN ? (MI > 1 ? 1 : 0) : MI / WN;
     const int token = 8 * (lane / 32) + lane % 16 / 4, feature = 16 * (lane / 16 % 2) + 4 * (lane % 4);
-    const int a_lane = token * A_PITCH + wm * (BM / WM) + feature, b_lane = P * A_SIZE + token * B_PITCH + wn * (BN / WN) + feature;
+    auto block = [&](int i) { return (i + wn * TURN) % MI; };
+    int a_lane[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) a_lane[i] = token * A_PITCH + wm * (BM / WM) + feature + block(i) * 32;
+    const int b_lane = P * A_SIZE + token * B_PITCH + wn * (BN / WN) + feature;
     auto operand = [&](const uint16_t *at, int pitch) {
         typedef __attribute__((address_space(3))) S4 Lds;
         const S4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds *)(at));
@@ -182,11 +207,10 @@ template <typename T, int BM, int BN, int BK, bool SMALL> __global__ __launch_bo
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int i = 0; i < MI; ++i) xa[set][p][i] = operand(from + a_lane + p * A_SIZE + step * 16 * A_PITCH + i * 32, A_PITCH);
+            for (int i = 0; i < MI; ++i)
+                xa[set][p][i] = operand(from + a_lane[i] + p * A_SIZE + step * 16 * A_PITCH, A_PITCH);
     };
     F16v acc[MI][NI] = {};
-    // Sums of dY over the tokens.  Two wavefronts hold the same operands: of two blocks of 32 features the one sums the first, the other the second.
-    constexpr int CI = (MI + 1) / 2;
     float colsum[CI] = {};
     auto multiply = [&](int set) {
 #pragma unroll
@@ -197,43 +221,69 @@ template <typename T, int BM, int BN, int BK, bool SMALL> __global__ __launch_bo
                 for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[set][p][i], xb[set][j], acc[i][j], 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < CI; ++i) {
-                const U4 first = __builtin_bit_cast(U4, xa[set][p][2 * i]), second = __builtin_bit_cast(U4, xa[set][p][2 * i + 1 < MI ? 2 * i + 1 : 2 * i]);
+                const U4 d = __builtin_bit_cast(U4, xa[set][p][i]);
                 const Pair one = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t d = wn == 0 ? first[j] : second[j];
-                    colsum[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair, d), one, colsum[i], false);
+                    const uint32_t two = d[j];
+                    colsum[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair, two), one, colsum[i], false);
                 }
             }
         }
     };
 
-    fetch(row0);
-    stage(lds, 0, 1);
-    fetch(row0 + BK);
+    using Yes = std::true_type;
+    using No = std::false_type;
+    int64_t row = row0;
+    fetch(No(), 0, row, 0, 1);
+    stage(0, lds, 0, 1);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fetch(No(), i, row + (i + 1) * BK, 0, 1);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): in the loop the loads come back in the loop's own order, and waits there count on it
     __syncthreads();
     take(lds, 0, 0);
     int cur = 0;
-    for (int64_t row = row0; row < row_end; row += BK) {
+    // A tile: operands of the step after next are read, a part of the next tile is converted and the same part of the one behind it asked for, while
+    // the matrix instructions of a step run.
+    auto tile_of = [&](auto within, int set) {
         uint16_t *const now = lds + cur, *const next = lds + (BUFFER - cur);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             if (s + 1 < STEPS) {
                 take(now, s + 1, (s + 1) % 2);
-                stage(next, s, STEPS - 1);
+                stage(set, next, s, STEPS - 1);
+                fetch(within, set, row + (AHEAD + 1) * BK, s, STEPS - 1);
             } else {
-                fetch(row + 2 * BK);
                 __syncthreads();
                 take(next, 0, (s + 1) % 2);
             }
             multiply(s % 2);
+#pragma unroll
+            for (int g = 0; g < P * MI * NI; ++g) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+                __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            }
         }
         cur = BUFFER - cur;
+        row += BK;
+    };
+    if constexpr (!SMALL)
+        while (row + (2 * AHEAD + 1) * BK <= row_end) {
+#pragma unroll
+            for (int set = 0; set < AHEAD; ++set) tile_of(Yes(), set);
+        }
+    while (row < row_end) {
+#pragma unroll
+        for (int set = 0; set < AHEAD; ++set)
+            if (set == 0 || row < row_end) tile_of(No(), set);
     }
 #pragma unroll
     for (int i = 0; i < CI; ++i) {
         const float t = colsum[i] + __shfl_xor(colsum[i], 32);
-        if (lane < 32 && (wn == 0 || 2 * i + 1 < MI)) sums[wm * (BM / WM) + (2 * i + wn) * 32 + lane] = t;
+        if (lane < 32 && wn * CI < MI) sums[wm * (BM / WM) + block(i) * 32 + lane] = t;
     }
     __syncthreads();
     const bool last = f.split == 1;
@@ -254,7 +304,7 @@ template <typename T, int BM, int BN, int BK, bool SMALL> __global__ __launch_bo
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int q = 0; q < 16; ++q) {
-                const int m = wm * (BM / WM) + i * 32 + 8 * (q / 4) + 4 * (lane / 32) + q % 4;
+                const int m = wm * (BM / WM) + block(i) * 32 + 8 * (q / 4) + 4 * (lane / 32) + q % 4;
                 if (out0 + m >= f.n_out || out0 + m < own_out) continue;
                 float *at = to + (out0 + m) * f.n_in + c;
                 float t = acc[i][j][q];
@@ -268,20 +318,64 @@ template <typename T, int BM, int BN, int BK, bool SMALL> __global__ __launch_bo
     }
 }
 
-// The partial products added up, weight and bias applied.
-__global__ __launch_bounds__(256) void k_weight_join(Product f, int dt_is_f16, int wide) {
-    const unsigned blocks = static_cast<unsigned>((f.n_in + 255) / 256);  // of a row
-    const int64_t n = blockIdx.x / blocks, k = static_cast<int64_t>(blockIdx.x % blocks) * 256 + threadIdx.x;
-    float bias_sum = 0.f;
-    for (int s = 0; s < f.split; ++s) bias_sum += f.partial_db[s * f.n_out + n];
-    if (k == 0 && f.db != nullptr) f.db[n] = bias_sum + (f.accumulate != 0 ? f.db[n] : 0.f);
-    if (k >= f.n_in) return;
-    float t = 0.f;
-    for (int s = 0; s < f.split; ++s) t += f.partial[(s * f.n_out + n) * f.n_in + k];
-    if (f.weight != nullptr) t *= weight_at(f.weight, wide != 0, dt_is_f16, k, 1.f);
-    if (f.bias != nullptr) t = __builtin_fmaf(bias_sum, weight_at(f.bias, wide != 0, dt_is_f16, k, 0.f), t);
-    float *at = f.dw + n * f.n_in + k;
-    *at = t + (f.accumulate != 0 ? *at : 0.f);
+// The partial products added up in the order of the tokens, weight and bias applied.  Four results per thread, wherever rows end.
+struct Join {
+    Product f;
+    Divisor per_row;  // n_in
+    int f16;
+};
+__global__ __launch_bounds__(256) void k_weight_join(Join w) {
+    const Product &f = w.f;
+    typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+    const int64_t all = f.n_out * f.n_in;
+    const uint32_t first = (blockIdx.x * 256u + threadIdx.x) * 4u;
+    if (first < f.n_out && f.db != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (first + j >= f.n_out) break;
+            float t = 0.f;
+            for (int s = 0; s < f.split; ++s) t += f.partial_db[s * f.n_out + first + j];
+            f.db[first + j] = t + (f.accumulate != 0 ? f.db[first + j] : 0.f);
+        }
+    }
+    if (first >= all) return;
+    float t[4] = {};
+    const bool whole = first + 4 <= all;
+    for (int s = 0; s < f.split; ++s) {
+        const float *from = f.partial + s * all + first;
+        if (whole) {
+            const F4 v = *reinterpret_cast<const F4 *>(from);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t[j] += v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (first + j < all) t[j] += from[j];
+        }
+    }
+    if (f.weight != nullptr || f.bias != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t n = w.per_row.quotient(first + j), k = first + j - n * w.per_row.d;
+            if (first + j >= all) break;
+            if (f.weight != nullptr) t[j] *= weight_at(f.weight, f.wide_weight, w.f16, k, 1.f);
+            if (f.bias != nullptr) {
+                float sum = 0.f;
+                for (int s = 0; s < f.split; ++s) sum += f.partial_db[s * f.n_out + n];
+                t[j] = __builtin_fmaf(sum, weight_at(f.bias, f.wide_weight, w.f16, k, 0.f), t[j]);
+            }
+        }
+    }
+    float *to = f.dw + first;
+    if (whole) {
+        F4 v = {t[0], t[1], t[2], t[3]};
+        if (f.accumulate != 0) v += *reinterpret_cast<const F4 *>(to);
+        *reinterpret_cast<F4 *>(to) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (first + j < all) to[j] = t[j] + (f.accumulate != 0 ? to[j] : 0.f);
+    }
 }
 
 // Tiles that there are kernels for, as (BM, BN).
@@ -295,25 +389,36 @@ struct Cut {
     int tiles_in, tiles, split;
     int64_t rows_per_split;
 };
-Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in, bool far) {
+// What a step of 64 tokens takes, us, with one workgroup on a compute unit and with as many as fit (two of the smaller tiles, but for fp32), by the
+// pieces of dY (bf16, fp16, fp32) and by tile; and what a workgroup takes beside its steps.  Measured over 1024 and 4096 tokens with 256 and 512
+// workgroups.  The larger tiles do two and a half times the work per time of the 64 x 64, but there are fewer of them: which tile and how many shares
+// of the tokens are best is the least of the sums below.
+constexpr float STEP_ALONE[3][TILES] = {{1.93f, 1.46f, 1.09f, 1.06f, 0.37f, 0.5f}, {3.3f, 0.f, 2.27f, 1.45f, 0.64f, 0.9f}, {4.78f, 0.f, 3.06f, 1.89f, 0.87f, 1.2f}};
+constexpr float STEP_FULL[3][TILES] = {{1.93f, 1.46f, 1.09f, 1.31f, 0.58f, 0.8f}, {3.3f, 0.f, 2.27f, 2.46f, 1.02f, 1.4f}, {4.78f, 0.f, 3.06f, 1.89f, 0.87f, 1.2f}};
+constexpr float BESIDE[TILES] = {22.f, 20.f, 14.f, 12.f, 6.f, 6.f};
+constexpr int SPLIT_MAX = 16;
+int per_unit(int tile, int pieces) { return tile < TILE_128_128 || pieces == 3 ? 1 : 2; }  // (fp32's tiles take the LDS of one)
+
+Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, bool far) {
     Cut best{};
     double least = 0;
+    const int pieces = dt == ADATOPK_BF16 ? 1 : (dt == ADATOPK_F16 ? 2 : 3);
     const int64_t steps = rows > 0 ? (rows + SHARE - 1) / SHARE : 1;
     for (int t = 0; t < TILES; ++t) {
         const bool fits = n_out >= TILE_BM[t] && adatopk_internal::act8_pitch(n_in) >= TILE_BN[t] && !far;
-        if (t != TILE_SMALL && !fits) continue;
-        if (t == TILE_SMALL && best.split != 0) continue;
+        if (t == TILE_SMALL ? best.split != 0 : !fits) continue;
+        if (t == TILE_256_192 && pieces != 1) continue;  // (its octets do not divide evenly in the shorter tiles of the other types)
         const int64_t in = (n_in + TILE_BN[t] - 1) / TILE_BN[t], tiles = in * ((n_out + TILE_BM[t] - 1) / TILE_BM[t]);
-        for (int64_t split = 1; split <= 16 && split <= steps; ++split) {
+        const int64_t places = 256 * per_unit(t, pieces);
+        for (int64_t split = 1; split <= SPLIT_MAX && split <= steps && (split == 1 || n_out * n_in < (static_cast<int64_t>(1) << 31)); ++split) {
             const int64_t per = (steps + split - 1) / split;
             if ((steps + per - 1) / per != split) continue;
-            const int per_unit = t >= TILE_64_64 ? 4 : t == TILE_128_128 ? 2 : 1;
-            const double area = static_cast<double>(TILE_BM[t]) * TILE_BN[t] / 65536.;
-            const double rounds = static_cast<double>((tiles * split + 256 * per_unit - 1) / (256 * per_unit));
-            const double step = (0.4 + 0.9 * area * per_unit) * per;
-            const double join = split == 1 ? 0 : 4.0 + static_cast<double>(split) * n_out * n_in * 8 / 4e6;
-            const double cost = rounds * (step + 4.0) + join;
-            if (least == 0 || cost < least) {
+            const int64_t full = tiles * split / places, rest = tiles * split % places;
+            const double alone = BESIDE[t] + static_cast<double>(STEP_ALONE[pieces - 1][t]) * per, together = BESIDE[t] + static_cast<double>(STEP_FULL[pieces - 1][t]) * per;
+            // partial products written and read, and a launch: 5 us and 0.4 us for each MB of a share's
+            const double join = split == 1 ? 0. : 5. + 0.4e-6 * 4. * static_cast<double>(split) * static_cast<double>(n_out * n_in);
+            const double cost = full * together + (rest == 0 ? 0. : rest <= 256 ? alone : together) + join;
+            if (best.split == 0 || cost < least) {
                 least = cost;
                 best = Cut{static_cast<Tile>(t), static_cast<int>(in), static_cast<int>(tiles), static_cast<int>(split), per * SHARE};
             }
@@ -337,7 +442,7 @@ size_t adatopk_weight_grad_workspace_bytes(int64_t rows, int64_t n_out, int64_t 
     if (n_out == 0 || n_in == 0) return 256;
     size_t most = 256;
     for (const bool far : {false, true}) {
-        const Cut c = cut_of(rows, n_out, n_in, far);
+        const Cut c = cut_of(rows, n_out, n_in, dt, far);
         const size_t bytes = static_cast<size_t>(c.split) * static_cast<size_t>(n_out) * (static_cast<size_t>(n_in) + 1) * sizeof(float);
         if (c.split > 1 && bytes > most) most = bytes;
     }
@@ -354,7 +459,7 @@ adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void
         !pointer_ok(workspace, 256) || (rows > 0 && (!matrix_ok(dy, dy_stride, rows, n_out, dt) || !pointer_ok(act8_x, 16))))
         return ADATOPK_EINVAL;
     if (workspace_bytes < adatopk_weight_grad_workspace_bytes(rows, n_out, n_in, dt)) return ADATOPK_EWORKSPACE;
-    const Cut c = cut_of(rows, n_out, n_in, rows > 1 && dy_stride >= MAX_STRIDE);
+    const Cut c = cut_of(rows, n_out, n_in, dt, rows > 1 && dy_stride >= MAX_STRIDE);
     float *partial = static_cast<float *>(workspace);
     const bool wide = weight_dt == ADATOPK_F32;
     const Product f{dy,     dy_stride, act8_of(const_cast<void *>(act8_x), rows, n_in), rows, n_out, n_in, c.rows_per_split, c.tiles_in, c.tiles, c.split,
@@ -363,17 +468,26 @@ adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void
     with_type(dt, [&](auto *null) {
         using T = std::remove_pointer_t<decltype(null)>;
         constexpr int DEEP = pieces_of<T>() == 1 ? 64 : 32;  // tokens of a tile: what two buffers have room for
-        const auto kernel = c.tile == TILE_256_256   ? k_weight_grad<T, 256, 256, DEEP, false>
-                            : c.tile == TILE_256_192 ? k_weight_grad<T, 256, 192, DEEP, false>
-                            : c.tile == TILE_256_128 ? k_weight_grad<T, 256, 128, DEEP, false>
-                            : c.tile == TILE_128_128 ? k_weight_grad<T, 128, 128, DEEP, false>
-                            : c.tile == TILE_64_64   ? k_weight_grad<T, 64, 64, DEEP, false>
-                                                     : k_weight_grad<T, 64, 64, DEEP, true>;
-        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(c.tiles * c.split)), dim3(NT), 0, st, f);
+        constexpr int SHALLOW = pieces_of<T>() == 1 ? 64 : 64;
+        const auto launch = [&](auto kernel, int threads) {
+            hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(c.tiles * c.split)), dim3(static_cast<unsigned>(threads)), 0, st, f);
+        };
+        if (c.tile == TILE_256_256)
+            launch(k_weight_grad<T, 256, 256, DEEP, 4, 2, 1, 1, false>, 512);
+        else if (c.tile == TILE_256_128)
+            launch(k_weight_grad<T, 256, 128, DEEP, 4, 2, 1, 1, false>, 512);
+        else if (c.tile == TILE_256_192) {
+            if constexpr (pieces_of<T>() == 1) launch(k_weight_grad<T, 256, 192, DEEP, 2, 2, 1, 1, false>, 256);
+        } else if (c.tile == TILE_128_128)
+            launch(k_weight_grad<T, 128, 128, 32, 2, 2, pieces_of<T>() < 3 ? 2 : 1, 1, false>, 256);
+        else if (c.tile == TILE_64_64)
+            launch(k_weight_grad<T, 64, 64, SHALLOW, 2, 2, pieces_of<T>() < 3 ? 2 : 1, 2, false>, 256);
+        else
+            launch(k_weight_grad<T, 64, 64, SHALLOW, 2, 2, pieces_of<T>() < 3 ? 2 : 1, 2, true>, 256);
     });
     if (c.split > 1)
-        hipLaunchKernelGGL(k_weight_join, dim3(static_cast<unsigned>((n_in + 255) / 256 * n_out)), dim3(256), 0, st, f,
-                           weight_dt == ADATOPK_F16 ? 1 : 0, wide ? 1 : 0);
+        hipLaunchKernelGGL(k_weight_join, dim3(static_cast<unsigned>((n_out * n_in + 1023) / 1024)), dim3(256), 0, st,
+                           Join{f, Divisor(static_cast<uint32_t>(n_in)), weight_dt == ADATOPK_F16 ? 1 : 0});
     return launched();
 }
 

@@ -140,3 +140,24 @@ def test_more_elements_than_32_bits_count():
     for n in (0, 1, 4_000, 7_499):
         column = dy[:, n].float()
         assert torch.equal(dw[n], (column[:, None] * x).sum(0)) and float(db[n]) == float(column.sum())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_larger_tiles_whole_numbers(dtype):
+    # products large enough for every tile that there is, with edges that are no multiples of it, and a token or two into a tile's tokens
+    for rows, n_out, n_in in ((130, 6400, 1600), (65, 4099, 4100), (257, 2000, 1700), (1029, 1030, 771), (64, 5000, 200), (193, 300, 3333), (33, 3001, 6001), (5000, 1281, 1601)):
+        gen = torch.Generator(device="cuda").manual_seed(rows)
+        dy = torch.randint(-4, 5, (rows, n_out + 8), device="cuda", generator=gen).to(dtype)[:, :n_out]
+        x = torch.randint(-3, 4, (rows, n_in), device="cuda", generator=gen).float()
+        w, b = (torch.randint(-2, 3, (n_in,), device="cuda", generator=gen).to(dtype) for _ in range(2))
+        buffer = B.new_act8(rows, n_in)
+        B.adatopk_act8_store(x, buffer)
+        dw, db = torch.full((n_out + 1, n_in), 9.0, device="cuda"), torch.empty(n_out, device="cuda")
+        ws = workspace(rows, n_out, n_in, dtype)
+        for affine in (False, True):
+            B.adatopk_weight_grad(dy, buffer, dw[:n_out], db, ws, weight=w if affine else None, bias=b if affine else None)
+            held = x.double() * w.double() + b.double() if affine else x.double()
+            assert torch.equal(dw[:n_out].double(), dy.double().t().contiguous() @ held), (rows, n_out, n_in, affine)
+            assert torch.equal(db.double(), dy.double().sum(0)) and bool((dw[n_out] == 9.0).all())
+        B.adatopk_weight_grad(dy, buffer, dw[:n_out], db, ws, accumulate=True)
+        assert torch.equal(dw[:n_out].double(), dy.double().t().contiguous() @ (held + x.double())), (rows, n_out, n_in)
