@@ -15,18 +15,20 @@ namespace {
 
 using namespace adatopk_stage;
 
-constexpr int SLOTS = 4;                   // octets per lane at most: 2048 elements per wavefront
-constexpr int WIDE_WAVES = 16;             // wavefronts of a row at most
-constexpr int64_t MAX_COLS = static_cast<int64_t>(SLOTS) * 512 * WIDE_WAVES;  // 32768
-constexpr int ROWS_PER_GROUP = 4;          // rows of a workgroup of one-wavefront rows
-constexpr int PARTS = 256;                 // workgroups that leave partial sums of the weight's gradient, at most
+constexpr int64_t MAX_COLS = 32768;        // 16 wavefronts with four octets per lane
+constexpr int COMPUTE_UNITS = 256;
+constexpr int WAVES = 8;                   // wavefronts of a workgroup, at most, where a row takes eight or fewer
 
-// Sum over the W wavefronts of a row, in every lane.  `scratch`: W floats per value in LDS.
+// Threads of the largest workgroup, and rows that one works on at a time: a team of W wavefronts to a row.
+template <int W> constexpr int threads_of() { return (W > WAVES ? W : WAVES) * 64; }
+template <int W> constexpr int teams_of() { return W > WAVES ? 1 : WAVES / W; }
+
+// Sum over the W wavefronts of a row, in every lane.  `scratch`: W floats per value in LDS, the team's own.  Every wavefront of the workgroup calls it.
 template <int W, int N> __device__ __forceinline__ void row_sum(float (&v)[N], float *scratch) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
     if constexpr (W > 1) {
-        const int wave = threadIdx.x / 64;
+        const int wave = threadIdx.x / 64 % W;
         __syncthreads();  // the scratch of the sum before has been read
         if (threadIdx.x % 64 == 0)
 #pragma unroll
@@ -64,62 +66,82 @@ template <typename T> __device__ __forceinline__ void load_weight(const void *p,
     }
 }
 
-// One row per W wavefronts (W > 1: per workgroup).
-template <typename T, int W, int S> __global__ __launch_bounds__(W > 1 ? W * 64 : ROWS_PER_GROUP * 64) void k_layernorm_forward(Forward f) {
-    __shared__ float scratch[2 * W];
-    const int lane = threadIdx.x % (W * 64);
-    const int64_t row = W > 1 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * ROWS_PER_GROUP + threadIdx.x / 64;
-    if (row >= f.rows) return;  // (a whole wavefront, or W == 1)
+// A workgroup's teams of W wavefronts take a row each, and rows come round in steps of the grid: weight and bias stay in registers, and the next row is on
+// its way while this one is summed up.
+template <typename T, int W, int S> __global__ __launch_bounds__(threads_of<W>()) void k_layernorm_forward(Forward f) {
+    __shared__ float scratch[teams_of<W>()][W];
+    const int lane = threadIdx.x % (W * 64), team = threadIdx.x / (W * 64);
+    const int64_t teams = blockDim.x / (W * 64), step = gridDim.x * teams;
     const float inverse = 1.f / static_cast<float>(f.cols);
-    float v[S][8];
-    float sums[1] = {0.f};
+    int64_t row = blockIdx.x * teams + team;
+    Raw<T> x[S], r[S];
+    auto fetch = [&](int64_t of) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = of < f.rows ? f.cols - at : 0;
+            x[s] = load_row(static_cast<const T *>(f.x) + of * f.x_stride + at, left);
+            if (f.residual != nullptr) r[s] = load_row(static_cast<const T *>(f.residual) + of * f.residual_stride + at, left);
+        }
+    };
+    fetch(row);
+    float w[S][8], b[S][8];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = f.cols - at;
-        unpack(load_row(static_cast<const T *>(f.x) + row * f.x_stride + at, left), v[s]);
-        if (f.residual != nullptr) {
-            float r[8];
-            unpack(load_row(static_cast<const T *>(f.residual) + row * f.residual_stride + at, left), r);
+        load_weight<T>(f.weight, f.wide_weight, at, left, 1.f, w[s]);
+        load_weight<T>(f.bias, f.wide_weight, at, left, 0.f, b[s]);
+    }
+    for (; row - team < f.rows; row += step) {  // (the workgroup's teams go round together, one without a row along with the others)
+        const bool there = row < f.rows;
+        float v[S][8];
+        float sums[1] = {0.f};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[s][j] += r[j];
-            const Raw<T> out = pack<T>(v[s]);
-            if (f.sum != nullptr) store_row(static_cast<T *>(f.sum) + row * f.sum_stride + at, left, out);
-            unpack(out, v[s]);
+        for (int s = 0; s < S; ++s) {
+            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = there ? f.cols - at : 0;
+            unpack(x[s], v[s]);
+            if (f.residual != nullptr) {
+                float t[8];
+                unpack(r[s], t);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[s][j] += t[j];
+                const Raw<T> out = pack<T>(v[s]);
+                if (f.sum != nullptr) store_row(static_cast<T *>(f.sum) + row * f.sum_stride + at, left, out);
+                unpack(out, v[s]);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[0] += v[s][j];
+        }
+        fetch(row + step);
+        row_sum<W>(sums, scratch[team]);
+        const float mean = sums[0] * inverse;
+        sums[0] = 0.f;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[s][j] = at + j < f.cols ? v[s][j] - mean : 0.f;
+                sums[0] = __builtin_fmaf(v[s][j], v[s][j], sums[0]);
+            }
+        }
+        row_sum<W>(sums, scratch[team]);
+        const float rstd = 1.f / __fsqrt_rn(sums[0] * inverse + f.eps);
+        if (lane == 0 && there) {
+            if (f.mean != nullptr) f.mean[row] = mean;
+            if (f.rstd != nullptr) f.rstd[row] = rstd;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sums[0] += v[s][j];
-    }
-    row_sum<W>(sums, scratch);
-    const float mean = sums[0] * inverse;
-    sums[0] = 0.f;
+        for (int s = 0; s < S; ++s) {
+            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = there ? f.cols - at : 0;
+            float y[8];
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[s][j] = at + j < f.cols ? v[s][j] - mean : 0.f;
-            sums[0] = __builtin_fmaf(v[s][j], v[s][j], sums[0]);
+            for (int j = 0; j < 8; ++j) {
+                v[s][j] *= rstd;
+                y[j] = __builtin_fmaf(v[s][j], w[s][j], b[s][j]);
+            }
+            store_row(static_cast<T *>(f.y) + row * f.y_stride + at, left, pack<T>(y));
+            if (f.act8.q != nullptr && there) act8_put(f.act8, row, static_cast<int>(at / 8), v[s]);
         }
-    }
-    row_sum<W>(sums, scratch);
-    const float rstd = 1.f / __fsqrt_rn(sums[0] * inverse + f.eps);
-    if (lane == 0) {
-        if (f.mean != nullptr) f.mean[row] = mean;
-        if (f.rstd != nullptr) f.rstd[row] = rstd;
-    }
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = f.cols - at;
-        float w[8], b[8];
-        load_weight<T>(f.weight, f.wide_weight, at, left, 1.f, w);
-        load_weight<T>(f.bias, f.wide_weight, at, left, 0.f, b);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[s][j] *= rstd;
-            b[j] = __builtin_fmaf(v[s][j], w[j], b[j]);
-        }
-        store_row(static_cast<T *>(f.y) + row * f.y_stride + at, left, pack<T>(b));
-        if (f.act8.q != nullptr) act8_put(f.act8, row, static_cast<int>(at / 8), v[s]);
     }
 }
 
@@ -134,76 +156,121 @@ struct Backward {
     Act8 act8;
 };
 
-// A workgroup takes rows blockIdx.x, blockIdx.x + gridDim.x, ... (W == 1: four at a time) and keeps its share of the weight's gradient in registers.
-template <typename T, int W, int S> __global__ __launch_bounds__(W > 1 ? W * 64 : ROWS_PER_GROUP * 64) void k_layernorm_backward(Backward f) {
-    __shared__ float scratch[2 * W];
-    const int lane = threadIdx.x % (W * 64);
-    const int64_t first = W > 1 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * ROWS_PER_GROUP + threadIdx.x / 64;
-    const int64_t step = W > 1 ? gridDim.x : static_cast<int64_t>(gridDim.x) * ROWS_PER_GROUP;
+// Rows come round as in the forward pass.  A row's operands stay as they were loaded and are taken apart twice, for the sums and for dx: half the
+// registers of keeping them as floats, which the next row's operands take.  KEEP: h comes from the 8-bit rows.
+template <typename T, int W, int S, bool KEEP> __global__ __launch_bounds__(threads_of<W>()) void k_layernorm_backward(Backward f) {
+    constexpr bool AHEAD = W <= WAVES;  // (sixteen wavefronts have half the registers each: they load a row when it is its turn)
+    __shared__ float scratch[teams_of<W>()][2 * W];
+    const int lane = threadIdx.x % (W * 64), team = threadIdx.x / (W * 64);
+    const int64_t teams = blockDim.x / (W * 64), step = gridDim.x * teams;
     const float inverse = 1.f / static_cast<float>(f.cols);
-    float dw[S][8] = {}, db[S][8] = {};
-    for (int64_t row = first; row < f.rows; row += step) {
-        float g[S][8], h[S][8];
-        float sums[2] = {0.f, 0.f};
-        const float rstd = f.rstd[row], mean = f.x != nullptr ? f.mean[row] : 0.f;
+    struct Row {
+        Raw<T> dy[S], ds[S], x[KEEP ? 1 : S];
+        U2 q[KEEP ? S : 1];
+        uint32_t e[KEEP ? S : 1];
+        float mean, rstd;
+    };
+    auto fetch = [&](Row &to, int64_t row) {
+        const bool there = row < f.rows;
+        to.rstd = there ? f.rstd[row] : 0.f;
+        to.mean = !KEEP && there ? f.mean[row] : 0.f;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = f.cols - at;
-            unpack(load_row(static_cast<const T *>(f.dy) + row * f.dy_stride + at, left), g[s]);
-            if (f.x != nullptr) {
-                unpack(load_row(static_cast<const T *>(f.x) + row * f.x_stride + at, left), h[s]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[s][j] = j < left ? (h[s][j] - mean) * rstd : 0.f;
+            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = there ? f.cols - at : 0;
+            to.dy[s] = load_row(static_cast<const T *>(f.dy) + row * f.dy_stride + at, left);
+            if constexpr (KEEP) {
+                if (left > 0) {
+                    act8_get(f.act8, row, static_cast<int>(at / 8), to.q[s], to.e[s]);
+                } else {
+                    to.q[s] = U2{0, 0};
+                    to.e[s] = 7;
+                }
             } else {
-                U2 d;
-                uint32_t E;
-                act8_get(f.act8, row, static_cast<int>(at / 8), d, E);
-                values_of(d, E, h[s]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[s][j] = j < left ? h[s][j] : 0.f;
+                to.x[s] = load_row(static_cast<const T *>(f.x) + row * f.x_stride + at, left);
             }
-            float w[8];
-            load_weight<T>(f.weight, f.wide_weight, at, left, 1.f, w);
+            if (f.dsum != nullptr) to.ds[s] = load_row(static_cast<const T *>(f.dsum) + row * f.dsum_stride + at, left);
+        }
+    };
+    float dw[S][8] = {}, db[S][8] = {}, w[S][8];
+    int64_t row = blockIdx.x * teams + team;
+    Row now;
+    if constexpr (AHEAD) fetch(now, row);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8;
+        load_weight<T>(f.weight, f.wide_weight, at, f.cols - at, 1.f, w[s]);
+    }
+    auto take = [&](const Row &from, int s, float (&g)[8], float (&h)[8]) {
+        unpack(from.dy[s], g);
+        if constexpr (KEEP) {
+            values_of(from.q[s], from.e[s], h);
+        } else {
+            unpack(from.x[s], h);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = (h[j] - from.mean) * from.rstd;
+        }
+        // (what lies behind the row is no value: without x there it would count as -mean, and a group that is marked as no number is so in its padding)
+        const int64_t left = f.cols - (static_cast<int64_t>(s) * W * 64 + lane) * 8;
+        if (left < 8)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = j < left ? h[j] : 0.f;
+    };
+    for (; row - team < f.rows; row += step) {  // (the workgroup's teams go round together, one without a row along with the others)
+        Row next;
+        fetch(AHEAD ? next : now, AHEAD ? row + step : row);
+        float sums[2] = {0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            float g[8], h[8];
+            take(now, s, g, h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                dw[s][j] = __builtin_fmaf(g[s][j], h[s][j], dw[s][j]);
-                db[s][j] += g[s][j];
-                g[s][j] *= w[j];
-                sums[0] += g[s][j];
-                sums[1] = __builtin_fmaf(g[s][j], h[s][j], sums[1]);
+                dw[s][j] = __builtin_fmaf(g[j], h[j], dw[s][j]);
+                db[s][j] += g[j];
+                g[j] *= w[s][j];
+                sums[0] += g[j];
+                sums[1] = __builtin_fmaf(g[j], h[j], sums[1]);
             }
         }
-        row_sum<W>(sums, scratch);
+        row_sum<W>(sums, scratch[team]);
         const float level = sums[0] * inverse, along = sums[1] * inverse;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = f.cols - at;
-            float add[8] = {};
-            if (f.dsum != nullptr) unpack(load_row(static_cast<const T *>(f.dsum) + row * f.dsum_stride + at, left), add);
+            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = row < f.rows ? f.cols - at : 0;
+            float g[8], h[8], add[8] = {};
+            take(now, s, g, h);
+            if (f.dsum != nullptr) unpack(now.ds[s], add);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) add[j] += rstd * (g[s][j] - level - h[s][j] * along);
+            for (int j = 0; j < 8; ++j) add[j] += now.rstd * (g[j] * w[s][j] - level - h[j] * along);
             store_row(static_cast<T *>(f.dx) + row * f.dx_stride + at, left, pack<T>(add));
         }
+        if constexpr (AHEAD) now = next;
     }
     if (f.partial == nullptr) return;
-    if constexpr (W == 1) {  // the four rows' shares, in a fixed order
-        __shared__ float share[ROWS_PER_GROUP][512 + 8];
-        const int wave = threadIdx.x / 64;
-        for (int which = 0; which < 2; ++which)
+    if constexpr (teams_of<W>() > 1) {  // the teams' shares, in a fixed order
+        __shared__ float share[teams_of<W>()][S * W * 512];
+        const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
 #pragma unroll
-            for (int s = 0; s < S; ++s) {
-                __syncthreads();
+        for (int which = 0; which < 2; ++which) {
+            if (which != 0) __syncthreads();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) share[wave][j * 64 + lane] = which == 0 ? dw[s][j] : db[s][j];
-                __syncthreads();
-                for (int i = threadIdx.x; i < 512; i += ROWS_PER_GROUP * 64) {
-                    const int64_t col = static_cast<int64_t>(s) * 512 + (i % 64) * 8 + i / 64;
-                    float t = 0.f;
+            for (int s = 0; s < S; ++s)
 #pragma unroll
-                    for (int w = 0; w < ROWS_PER_GROUP; ++w) t += share[w][i];
-                    if (col < f.cols) f.partial[(blockIdx.x * static_cast<int64_t>(2) + which) * f.cols + col] = t;
-                }
+                for (int j = 0; j < 8; ++j) share[team][(s * 8 + j) * W * 64 + lane] = which == 0 ? dw[s][j] : db[s][j];
+            __syncthreads();
+            for (int piece = wave; piece < 2 * S * W; piece += waves) {  // four of the eight columns of 64 lanes' octets
+                const int s = piece / (2 * W), l = piece / 2 % W * 64 + threadIdx.x % 64, j0 = piece % 2 * 4;
+                float t[4] = {};
+                for (int v = 0; v < teams; ++v)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) t[j] += share[v][(s * 8 + j0 + j) * W * 64 + l];
+                const int64_t col = (static_cast<int64_t>(s) * W * 64 + l) * 8 + j0;
+                float *to = f.partial + (blockIdx.x * static_cast<int64_t>(2) + which) * f.cols + col;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (col + j < f.cols) to[j] = t[j];
             }
+        }
     } else {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
@@ -217,51 +284,54 @@ template <typename T, int W, int S> __global__ __launch_bounds__(W > 1 ? W * 64 
     }
 }
 
-// Columns of the partial sums added up, in a fixed order: 64 columns per workgroup, 16 lanes of parts for each.
+// Columns of the partial sums added up, in a fixed order: 32 columns per workgroup, 32 lanes of parts for each.
 __global__ __launch_bounds__(1024) void k_layernorm_join(const float *partial, int parts, int64_t cols, float *dweight, float *dbias, int accumulate) {
-    __shared__ float share[16][64];
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x % 64;  // column of the [2][cols] sums
-    const int lane = threadIdx.x / 64;
+    __shared__ float share[32][33];
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.x % 32;  // column of the [2][cols] sums
+    const int lane = threadIdx.x / 32;
     float t = 0.f;
-    if (i < 2 * cols)
-        for (int p = lane; p < parts; p += 16) t += partial[static_cast<int64_t>(p) * 2 * cols + i];
-    share[lane][threadIdx.x % 64] = t;
+    if (i < 2 * cols) {
+#pragma unroll 8
+        for (int p = lane; p < parts; p += 32) t += partial[static_cast<int64_t>(p) * 2 * cols + i];
+    }
+    share[lane][threadIdx.x % 32] = t;
     __syncthreads();
     if (lane != 0 || i >= 2 * cols) return;
     t = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) t += share[k][threadIdx.x];
+    for (int k = 0; k < 32; ++k) t += share[k][threadIdx.x];
     float *to = i < cols ? dweight : dbias;
     if (to == nullptr) return;
     to += i < cols ? i : i - cols;
     *to = accumulate != 0 ? *to + t : t;
 }
 
-// The smallest of the shapes that hold a row: f is called with W and S as types.
+// Wavefronts to a row and octets per lane that hold a row: f is called with W and S as types.  Two octets per lane leave room in the registers for the row
+// behind and the weight's gradient.
 template <int N> using Int = std::integral_constant<int, N>;
 template <typename F> void with_shape(int64_t cols, F &&f) {
-    if (cols <= 512)
-        f(Int<1>(), Int<1>());
-    else if (cols <= 1024)
-        f(Int<1>(), Int<2>());
-    else if (cols <= 2048)
-        f(Int<1>(), Int<4>());
-    else if (cols <= 4096)
-        f(Int<4>(), Int<2>());
-    else if (cols <= 8192)
-        f(Int<4>(), Int<4>());
-    else if (cols <= 16384)
-        f(Int<16>(), Int<2>());
-    else
-        f(Int<16>(), Int<4>());
+    if (cols <= 512) return f(Int<1>(), Int<1>());
+    if (cols <= 1024) return f(Int<1>(), Int<2>());
+    if (cols <= 2048) return f(Int<2>(), Int<2>());
+    if (cols <= 4096) return f(Int<4>(), Int<2>());
+    if (cols <= 8192) return f(Int<8>(), Int<2>());
+    if (cols <= 16384) return f(Int<16>(), Int<2>());
+    return f(Int<16>(), Int<4>());
 }
 
-bool wave_rows(int64_t cols) { return cols <= 2048; }
-// Workgroups of the backward pass, which is also how many partial sums there are.
-int64_t parts_of(int64_t rows, int64_t cols) {
-    const int64_t groups = wave_rows(cols) ? (rows + ROWS_PER_GROUP - 1) / ROWS_PER_GROUP : rows;
-    return groups < PARTS * 2 ? groups : PARTS * 2;
+// Wavefronts and workgroups of a launch: as many rows to a workgroup as it has teams for, but fewer where that would leave compute units without one.
+struct Launch {
+    int waves, groups;
+};
+Launch launch_of(int64_t rows, int waves_per_row, int groups_per_unit) {
+    int teams = waves_per_row < WAVES ? WAVES / waves_per_row : 1;
+    while (teams > 1 && rows < static_cast<int64_t>(COMPUTE_UNITS) * teams) teams /= 2;
+    const int64_t groups = (rows + teams - 1) / teams, most = static_cast<int64_t>(COMPUTE_UNITS) * groups_per_unit;
+    return Launch{teams * waves_per_row, static_cast<int>(groups < most ? groups : most)};
 }
+// Of the backward pass: as many partial sums as workgroups.
+Launch backward_launch(int64_t rows, int waves_per_row) { return launch_of(rows, waves_per_row, 1); }
+int64_t parts_at_most(int64_t rows) { return rows < COMPUTE_UNITS ? rows : COMPUTE_UNITS; }
 
 bool weights_ok(const void *p, adatopk_dtype wdt) { return pointer_ok_or_null(p, static_cast<size_t>(elem_size(wdt))); }
 
@@ -281,12 +351,12 @@ adatopk_status adatopk_layernorm_forward(const void *x, int64_t x_stride, const 
         return ADATOPK_EINVAL;
     const Forward f{x,        residual,        weight,     bias,     sum,  y,    mean, rstd,
                     x_stride, residual_stride, sum_stride, y_stride, rows, cols, eps,  weight_dt != dt, act8_of(act8, rows, cols)};
-    const int64_t groups = wave_rows(cols) ? (rows + ROWS_PER_GROUP - 1) / ROWS_PER_GROUP : rows;
     with_type(dt, [&](auto *null) {
         using T = std::remove_pointer_t<decltype(null)>;
         with_shape(cols, [&](auto waves, auto slots) {
             constexpr int W = decltype(waves)::value, S = decltype(slots)::value;
-            hipLaunchKernelGGL((k_layernorm_forward<T, W, S>), dim3(static_cast<unsigned>(groups)), dim3(W > 1 ? W * 64 : ROWS_PER_GROUP * 64), 0,
+            const Launch l = launch_of(rows, W, 2);
+            hipLaunchKernelGGL((k_layernorm_forward<T, W, S>), dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.waves * 64)), 0,
                                static_cast<hipStream_t>(hip_stream), f);
         });
     });
@@ -295,7 +365,7 @@ adatopk_status adatopk_layernorm_forward(const void *x, int64_t x_stride, const 
 
 size_t adatopk_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols) {
     if (!shape_ok(rows, cols) || cols > MAX_COLS) return 0;
-    return align_up(static_cast<size_t>(parts_of(rows, cols)) * 2 * static_cast<size_t>(cols) * sizeof(float), 256);
+    return align_up(static_cast<size_t>(parts_at_most(rows)) * 2 * static_cast<size_t>(cols) * sizeof(float), 256);
 }
 
 adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *act8, const float *mean,
@@ -313,7 +383,7 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
         return ADATOPK_EINVAL;
     if (weights && rows > 0 && workspace_bytes < adatopk_layernorm_backward_workspace_bytes(rows, cols)) return ADATOPK_EWORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const int64_t parts = parts_of(rows, cols);
+    int parts = 0;
     float *partial = weights ? static_cast<float *>(workspace) : nullptr;
     if (rows > 0) {
         const Backward f{dy,        x,        weight,      dsum,      mean, rstd, dx,
@@ -322,12 +392,15 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
             using T = std::remove_pointer_t<decltype(null)>;
             with_shape(cols, [&](auto waves, auto slots) {
                 constexpr int W = decltype(waves)::value, S = decltype(slots)::value;
-                hipLaunchKernelGGL((k_layernorm_backward<T, W, S>), dim3(static_cast<unsigned>(parts)), dim3(W > 1 ? W * 64 : ROWS_PER_GROUP * 64), 0, st, f);
+                const Launch l = backward_launch(rows, W);
+                parts = l.groups;
+                const auto kernel = act8 != nullptr ? k_layernorm_backward<T, W, S, true> : k_layernorm_backward<T, W, S, false>;
+                hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.waves * 64)), 0, st, f);
             });
         });
     }
     if (weights)  // (no rows: the sums are zero)
-        hipLaunchKernelGGL(k_layernorm_join, dim3(static_cast<unsigned>((2 * cols + 63) / 64)), dim3(1024), 0, st, partial, static_cast<int>(parts), cols,
+        hipLaunchKernelGGL(k_layernorm_join, dim3(static_cast<unsigned>((2 * cols + 31) / 32)), dim3(1024), 0, st, partial, parts, cols,
                            dweight, dbias, accumulate);
     return launched();
 }
