@@ -77,7 +77,7 @@ template <typename T> __global__ __launch_bounds__(NT) void k_act8_store(const T
     if (t >= s.octets) return;
     const uint32_t row = s.per_row.quotient(t), octet = t - row * s.per_row.d;
     float v[8];
-    unpack(load_row(x + row * stride + octet * static_cast<int64_t>(8), s.cols - octet * static_cast<int64_t>(8)), v);
+    unpack(load_row(x + row * stride + octet * static_cast<int64_t>(8), s.cols - octet * static_cast<int64_t>(8), octet > 0), v);
     act8_put(a, row, static_cast<int>(octet), v);
 }
 
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(NT) void k_gelu_forward(const T *x, int64_t x_strid
     const uint32_t row = s.per_row.quotient(t), octet = t - row * s.per_row.d;
     const int64_t at = octet * static_cast<int64_t>(8), left = s.cols - at;
     float v[8], g[8];
-    unpack(load_row(x + row * x_stride + at, left), v);
+    unpack(load_row(x + row * x_stride + at, left, at > 0), v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) g[j] = F::value(v[j]);
     const Raw<T> out = pack<T>(g);
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(NT) void k_gelu_backward(const T *dy, int64_t dy_st
     uint32_t E;
     act8_get(a, row, static_cast<int>(octet), d, E);
     float v[8], g[8];
-    unpack(load_row(dy + row * dy_stride + at, left), g);
+    unpack(load_row(dy + row * dy_stride + at, left, at > 0), g);
     values_of(d, E, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) g[j] *= F::slope(v[j]);

@@ -5,8 +5,8 @@
 //   backward  g = dy * weight;  dx = rstd * (g - sum g / n - h * (sum g h) / n) + dsum;  dweight = sum over rows dy * h;  dbias = sum over rows dy
 //             with h from the kept 8-bit rows, or from x, mean and rstd
 //
-// A row is read once and held in registers between the sums and their use: W wavefronts share it, an octet per lane and slot.  All sums are
-// in 32 bits and in a fixed order.
+// A row is read once and held in registers between the sums and their use (rows of more than 8192 elements are read again by the backward pass).  All sums
+// are in 32 bits and in a fixed order.
 #include <hip/hip_runtime.h>
 
 #include "stage_ops.h"
@@ -15,19 +15,31 @@ namespace {
 
 using namespace adatopk_stage;
 
-constexpr int64_t MAX_COLS = 32768;        // 16 wavefronts with four octets per lane
 constexpr int COMPUTE_UNITS = 256;
-constexpr int WAVES = 8;                   // wavefronts of a workgroup, at most, where a row takes eight or fewer
+constexpr int64_t MAX_COLS = 32768;        // 1024 lanes with four octets each
+// Threads of the largest workgroup, by the lanes to a row.
+constexpr int threads_of(int lanes) { return lanes < 512 ? 512 : lanes; }
 
-// Threads of the largest workgroup, and rows that one works on at a time: a team of W wavefronts to a row.
-template <int W> constexpr int threads_of() { return (W > WAVES ? W : WAVES) * 64; }
-template <int W> constexpr int teams_of() { return W > WAVES ? 1 : WAVES / W; }
-
-// Sum over the W wavefronts of a row, in every lane.  `scratch`: W floats per value in LDS, the team's own.  Every wavefront of the workgroup calls it.
-template <int W, int N> __device__ __forceinline__ void row_sum(float (&v)[N], float *scratch) {
+// A row is a team's: L lanes, from an eighth of a wavefront to a whole workgroup.  Sum over them, in a fixed order, in every lane; `scratch`: a float per
+// wavefront and value in LDS, the team's own.  Every lane of the workgroup calls it.
+template <int CONTROL> __device__ __forceinline__ float moved(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xF, 0xF, false));
+}
+template <int L, int N> __device__ __forceinline__ void team_sum(float (&v)[N], float *scratch) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
-    if constexpr (W > 1) {
+    for (int i = 0; i < N; ++i) {
+        if constexpr (L >= 64) {
+            v[i] = wave_sum(v[i]);
+        } else {
+            v[i] += moved<0xB1>(v[i]);   // the neighbour, the other pair of the quad, the other quad of eight lanes, the other half of sixteen
+            v[i] += moved<0x4E>(v[i]);
+            v[i] += moved<0x141>(v[i]);
+            if constexpr (L >= 16) v[i] += moved<0x140>(v[i]);
+            if constexpr (L >= 32) v[i] += __shfl_xor(v[i], 16);
+        }
+    }
+    if constexpr (L > 64) {
+        constexpr int W = L / 64;
         const int wave = threadIdx.x / 64 % W;
         __syncthreads();  // the scratch of the sum before has been read
         if (threadIdx.x % 64 == 0)
@@ -43,6 +55,8 @@ template <int W, int N> __device__ __forceinline__ void row_sum(float (&v)[N], f
         }
     }
 }
+// Up to two octets per lane, the row behind is loaded while one is summed up, and the weights stay in registers; with more, neither: a row is read again.
+constexpr bool held(int slots) { return slots <= 2; }
 
 struct Forward {
     const void *x, *residual, *weight, *bias;
@@ -60,44 +74,53 @@ template <typename T> __device__ __forceinline__ void load_weight(const void *p,
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = absent;
     } else if (wide) {
-        unpack(load_row(static_cast<const float *>(p) + at, left), v);
+        unpack(load_row(static_cast<const float *>(p) + at, left, at > 0), v);
     } else {
-        unpack(load_row(static_cast<const T *>(p) + at, left), v);
+        unpack(load_row(static_cast<const T *>(p) + at, left, at > 0), v);
     }
 }
 
-// A workgroup's teams of W wavefronts take a row each, and rows come round in steps of the grid: weight and bias stay in registers, and the next row is on
-// its way while this one is summed up.
-template <typename T, int W, int S> __global__ __launch_bounds__(threads_of<W>()) void k_layernorm_forward(Forward f) {
-    __shared__ float scratch[teams_of<W>()][W];
-    const int lane = threadIdx.x % (W * 64), team = threadIdx.x / (W * 64);
-    const int64_t teams = blockDim.x / (W * 64), step = gridDim.x * teams;
+// A workgroup's teams take a row each, and rows come round in steps of the grid: weight and bias stay in registers, and the next row is on its way while this
+// one is summed up.
+template <typename T, int L, int S> __global__ __launch_bounds__(threads_of(L)) void k_layernorm_forward(Forward f) {
+    constexpr bool HELD = held(S);
+    __shared__ float scratch[threads_of(L) / L][L > 64 ? L / 64 : 1];
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int64_t teams = blockDim.x / L, step = gridDim.x * teams;
     const float inverse = 1.f / static_cast<float>(f.cols);
     int64_t row = blockIdx.x * teams + team;
+    auto place = [&](int s) {  // (rows that are not held: what is derived from it is not kept from row to row either)
+        int l = lane;
+        if constexpr (!HELD) asm volatile("" : "+v"(l));
+        return (static_cast<int64_t>(s) * L + l) * 8;
+    };
     Raw<T> x[S], r[S];
     auto fetch = [&](int64_t of) {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = of < f.rows ? f.cols - at : 0;
-            x[s] = load_row(static_cast<const T *>(f.x) + of * f.x_stride + at, left);
-            if (f.residual != nullptr) r[s] = load_row(static_cast<const T *>(f.residual) + of * f.residual_stride + at, left);
+            const int64_t at = place(s), left = of < f.rows ? f.cols - at : 0;
+            x[s] = load_row(static_cast<const T *>(f.x) + of * f.x_stride + at, left, at > 0);
+            if (f.residual != nullptr) r[s] = load_row(static_cast<const T *>(f.residual) + of * f.residual_stride + at, left, at > 0);
         }
     };
-    fetch(row);
-    float w[S][8], b[S][8];
+    float w[HELD ? S : 1][8], b[HELD ? S : 1][8];
+    auto weights = [&](int s, int to) {
+        load_weight<T>(f.weight, f.wide_weight, place(s), f.cols - place(s), 1.f, w[to]);
+        load_weight<T>(f.bias, f.wide_weight, place(s), f.cols - place(s), 0.f, b[to]);
+    };
+    if constexpr (HELD) {
+        fetch(row);
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = f.cols - at;
-        load_weight<T>(f.weight, f.wide_weight, at, left, 1.f, w[s]);
-        load_weight<T>(f.bias, f.wide_weight, at, left, 0.f, b[s]);
+        for (int s = 0; s < S; ++s) weights(s, s);
     }
     for (; row - team < f.rows; row += step) {  // (the workgroup's teams go round together, one without a row along with the others)
         const bool there = row < f.rows;
+        if constexpr (!HELD) fetch(row);
         float v[S][8];
         float sums[1] = {0.f};
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = there ? f.cols - at : 0;
+            const int64_t at = place(s), left = there ? f.cols - at : 0;
             unpack(x[s], v[s]);
             if (f.residual != nullptr) {
                 float t[8];
@@ -111,20 +134,19 @@ template <typename T, int W, int S> __global__ __launch_bounds__(threads_of<W>()
 #pragma unroll
             for (int j = 0; j < 8; ++j) sums[0] += v[s][j];
         }
-        fetch(row + step);
-        row_sum<W>(sums, scratch[team]);
+        if constexpr (HELD) fetch(row + step);
+        team_sum<L>(sums, scratch[team]);
         const float mean = sums[0] * inverse;
         sums[0] = 0.f;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[s][j] = at + j < f.cols ? v[s][j] - mean : 0.f;
+                v[s][j] = place(s) + j < f.cols ? v[s][j] - mean : 0.f;
                 sums[0] = __builtin_fmaf(v[s][j], v[s][j], sums[0]);
             }
         }
-        row_sum<W>(sums, scratch[team]);
+        team_sum<L>(sums, scratch[team]);
         const float rstd = 1.f / __fsqrt_rn(sums[0] * inverse + f.eps);
         if (lane == 0 && there) {
             if (f.mean != nullptr) f.mean[row] = mean;
@@ -132,12 +154,14 @@ template <typename T, int W, int S> __global__ __launch_bounds__(threads_of<W>()
         }
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = there ? f.cols - at : 0;
+            const int64_t at = place(s), left = there ? f.cols - at : 0;
+            const int k = HELD ? s : 0;
+            if constexpr (!HELD) weights(s, 0);
             float y[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 v[s][j] *= rstd;
-                y[j] = __builtin_fmaf(v[s][j], w[s][j], b[s][j]);
+                y[j] = __builtin_fmaf(v[s][j], w[k][j], b[k][j]);
             }
             store_row(static_cast<T *>(f.y) + row * f.y_stride + at, left, pack<T>(y));
             if (f.act8.q != nullptr && there) act8_put(f.act8, row, static_cast<int>(at / 8), v[s]);
@@ -149,7 +173,9 @@ struct Backward {
     const void *dy, *x, *weight, *dsum;
     const float *mean, *rstd;
     void *dx;
-    float *partial;  // [parts][2][cols]: sums of dy * h and of dy over the rows of a workgroup
+    float *partial;  // [parts][2][cols]: sums of dy * h and of dy over the rows of a workgroup; or, from the only workgroup, nothing
+    float *dweight, *dbias;
+    int accumulate;
     int64_t dy_stride, x_stride, dsum_stride, dx_stride;
     int64_t rows, cols;
     bool wide_weight;
@@ -158,128 +184,162 @@ struct Backward {
 
 // Rows come round as in the forward pass.  A row's operands stay as they were loaded and are taken apart twice, for the sums and for dx: half the
 // registers of keeping them as floats, which the next row's operands take.  KEEP: h comes from the 8-bit rows.
-template <typename T, int W, int S, bool KEEP> __global__ __launch_bounds__(threads_of<W>()) void k_layernorm_backward(Backward f) {
-    constexpr bool AHEAD = W <= WAVES;  // (sixteen wavefronts have half the registers each: they load a row when it is its turn)
-    __shared__ float scratch[teams_of<W>()][2 * W];
-    const int lane = threadIdx.x % (W * 64), team = threadIdx.x / (W * 64);
-    const int64_t teams = blockDim.x / (W * 64), step = gridDim.x * teams;
+template <typename T, int L, int S, bool KEEP> __global__ __launch_bounds__(threads_of(L)) void k_layernorm_backward(Backward f) {
+    constexpr bool HELD = held(S);
+    constexpr int R = HELD ? S : 1;  // octets that are held at a time
+    __shared__ float scratch[threads_of(L) / L][L > 64 ? 2 * (L / 64) : 1];
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int64_t teams = blockDim.x / L, step = gridDim.x * teams;
     const float inverse = 1.f / static_cast<float>(f.cols);
+    auto place = [&](int s) {  // (rows that are not held: what is derived from it is not kept from row to row either)
+        int l = lane;
+        if constexpr (!HELD) asm volatile("" : "+v"(l));
+        return (static_cast<int64_t>(s) * L + l) * 8;
+    };
     struct Row {
-        Raw<T> dy[S], ds[S], x[KEEP ? 1 : S];
-        U2 q[KEEP ? S : 1];
-        uint32_t e[KEEP ? S : 1];
+        Raw<T> dy[R], ds[R], x[KEEP ? 1 : R];
+        U2 q[KEEP ? R : 1];
+        uint32_t e[KEEP ? R : 1];
         float mean, rstd;
     };
-    auto fetch = [&](Row &to, int64_t row) {
-        const bool there = row < f.rows;
-        to.rstd = there ? f.rstd[row] : 0.f;
-        to.mean = !KEEP && there ? f.mean[row] : 0.f;
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = there ? f.cols - at : 0;
-            to.dy[s] = load_row(static_cast<const T *>(f.dy) + row * f.dy_stride + at, left);
-            if constexpr (KEEP) {
-                if (left > 0) {
-                    act8_get(f.act8, row, static_cast<int>(at / 8), to.q[s], to.e[s]);
-                } else {
-                    to.q[s] = U2{0, 0};
-                    to.e[s] = 7;
-                }
-            } else {
-                to.x[s] = load_row(static_cast<const T *>(f.x) + row * f.x_stride + at, left);
-            }
-            if (f.dsum != nullptr) to.ds[s] = load_row(static_cast<const T *>(f.dsum) + row * f.dsum_stride + at, left);
-        }
+    auto scalars = [&](Row &to, int64_t row) {
+        to.rstd = row < f.rows ? f.rstd[row] : 0.f;
+        to.mean = !KEEP && row < f.rows ? f.mean[row] : 0.f;
     };
-    float dw[S][8] = {}, db[S][8] = {}, w[S][8];
+    auto fetch = [&](Row &to, int64_t row, int s, int at_slot, bool sum) {
+        const int64_t at = place(s), left = row < f.rows ? f.cols - at : 0;
+        to.dy[at_slot] = load_row(static_cast<const T *>(f.dy) + row * f.dy_stride + at, left, at > 0);
+        if constexpr (KEEP) {
+            if (left > 0) {
+                act8_get(f.act8, row, static_cast<int>(at / 8), to.q[at_slot], to.e[at_slot]);
+            } else {
+                to.q[at_slot] = U2{0, 0};
+                to.e[at_slot] = 7;
+            }
+        } else {
+            to.x[at_slot] = load_row(static_cast<const T *>(f.x) + row * f.x_stride + at, left, at > 0);
+        }
+        if (sum && f.dsum != nullptr) to.ds[at_slot] = load_row(static_cast<const T *>(f.dsum) + row * f.dsum_stride + at, left, at > 0);
+    };
+    auto fetch_all = [&](Row &to, int64_t row) {
+        scalars(to, row);
+#pragma unroll
+        for (int s = 0; s < R; ++s) fetch(to, row, s, s, true);
+    };
+    float dw[S][8] = {}, db[S][8] = {}, w[R][8];
+    auto weights = [&](int s, int to) { load_weight<T>(f.weight, f.wide_weight, place(s), f.cols - place(s), 1.f, w[to]); };
     int64_t row = blockIdx.x * teams + team;
     Row now;
-    if constexpr (AHEAD) fetch(now, row);
+    if constexpr (HELD) {
+        fetch_all(now, row);
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8;
-        load_weight<T>(f.weight, f.wide_weight, at, f.cols - at, 1.f, w[s]);
+        for (int s = 0; s < S; ++s) weights(s, s);
     }
-    auto take = [&](const Row &from, int s, float (&g)[8], float (&h)[8]) {
-        unpack(from.dy[s], g);
+    auto take = [&](const Row &from, int s, int slot, float (&g)[8], float (&h)[8]) {
+        unpack(from.dy[slot], g);
         if constexpr (KEEP) {
-            values_of(from.q[s], from.e[s], h);
+            values_of(from.q[slot], from.e[slot], h);
         } else {
-            unpack(from.x[s], h);
+            unpack(from.x[slot], h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = (h[j] - from.mean) * from.rstd;
         }
         // (what lies behind the row is no value: without x there it would count as -mean, and a group that is marked as no number is so in its padding)
-        const int64_t left = f.cols - (static_cast<int64_t>(s) * W * 64 + lane) * 8;
+        const int64_t left = f.cols - place(s);
         if (left < 8)
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = j < left ? h[j] : 0.f;
     };
     for (; row - team < f.rows; row += step) {  // (the workgroup's teams go round together, one without a row along with the others)
         Row next;
-        fetch(AHEAD ? next : now, AHEAD ? row + step : row);
+        if constexpr (HELD)
+            fetch_all(next, row + step);
+        else
+            scalars(now, row);
         float sums[2] = {0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < S; ++s) {
+            const int k = HELD ? s : 0;
+            if constexpr (!HELD) {
+                fetch(now, row, s, 0, false);
+                weights(s, 0);
+            }
             float g[8], h[8];
-            take(now, s, g, h);
+            take(now, s, k, g, h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 dw[s][j] = __builtin_fmaf(g[j], h[j], dw[s][j]);
                 db[s][j] += g[j];
-                g[j] *= w[s][j];
+                g[j] *= w[k][j];
                 sums[0] += g[j];
                 sums[1] = __builtin_fmaf(g[j], h[j], sums[1]);
             }
         }
-        row_sum<W>(sums, scratch[team]);
+        team_sum<L>(sums, scratch[team]);
         const float level = sums[0] * inverse, along = sums[1] * inverse;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = row < f.rows ? f.cols - at : 0;
+            const int k = HELD ? s : 0;
+            if constexpr (!HELD) {
+                fetch(now, row, s, 0, true);
+                weights(s, 0);
+            }
+            const int64_t at = place(s), left = row < f.rows ? f.cols - at : 0;
             float g[8], h[8], add[8] = {};
-            take(now, s, g, h);
-            if (f.dsum != nullptr) unpack(now.ds[s], add);
+            take(now, s, k, g, h);
+            if (f.dsum != nullptr) unpack(now.ds[k], add);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) add[j] += now.rstd * (g[j] * w[s][j] - level - h[j] * along);
+            for (int j = 0; j < 8; ++j) add[j] += now.rstd * (g[j] * w[k][j] - level - h[j] * along);
             store_row(static_cast<T *>(f.dx) + row * f.dx_stride + at, left, pack<T>(add));
         }
-        if constexpr (AHEAD) now = next;
+        if constexpr (HELD) now = next;
     }
-    if (f.partial == nullptr) return;
-    if constexpr (teams_of<W>() > 1) {  // the teams' shares, in a fixed order
-        __shared__ float share[teams_of<W>()][S * W * 512];
-        const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    if (f.dweight == nullptr && f.dbias == nullptr) return;
+    // n <= 8 neighbouring columns' sums: to the workgroup's place, or where there is but one, to where they belong
+    auto put = [&](int which, int64_t col, const float *t, int n) {
+        typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+        const bool only = gridDim.x == 1;
+        float *to = only ? (which == 0 ? f.dweight : f.dbias) : f.partial + (blockIdx.x * static_cast<int64_t>(2) + which) * f.cols;
+        if (to == nullptr) return;
+        to += col;
+        const bool add = only && f.accumulate != 0;
+#pragma unroll
+        for (int j = 0; j < n; j += 4) {
+            if (col + j + 4 <= f.cols) {
+                F4 v = {t[j], t[j + 1], t[j + 2], t[j + 3]};
+                if (add) v += *reinterpret_cast<const F4 *>(to + j);
+                *reinterpret_cast<F4 *>(to + j) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (col + j + i < f.cols) to[j + i] = t[j + i] + (add ? to[j + i] : 0.f);
+            }
+        }
+    };
+    if constexpr (L < threads_of(L)) {  // the teams' shares, in a fixed order
+        __shared__ float share[threads_of(L) / L][S * L * 8];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             if (which != 0) __syncthreads();
 #pragma unroll
             for (int s = 0; s < S; ++s)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) share[team][(s * 8 + j) * W * 64 + lane] = which == 0 ? dw[s][j] : db[s][j];
+                for (int j = 0; j < 8; ++j) share[team][(s * 8 + j) * L + lane] = which == 0 ? dw[s][j] : db[s][j];
             __syncthreads();
-            for (int piece = wave; piece < 2 * S * W; piece += waves) {  // four of the eight columns of 64 lanes' octets
-                const int s = piece / (2 * W), l = piece / 2 % W * 64 + threadIdx.x % 64, j0 = piece % 2 * 4;
+            for (int piece = threadIdx.x; piece < 2 * S * L; piece += blockDim.x) {  // four of the eight columns of an octet
+                const int octet = piece % (S * L), s = octet / L, l = octet % L, j0 = piece / (S * L) * 4;
                 float t[4] = {};
                 for (int v = 0; v < teams; ++v)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) t[j] += share[v][(s * 8 + j0 + j) * W * 64 + l];
-                const int64_t col = (static_cast<int64_t>(s) * W * 64 + l) * 8 + j0;
-                float *to = f.partial + (blockIdx.x * static_cast<int64_t>(2) + which) * f.cols + col;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (col + j < f.cols) to[j] = t[j];
+                    for (int j = 0; j < 4; ++j) t[j] += share[v][(s * 8 + j0 + j) * L + l];
+                put(which, static_cast<int64_t>(octet) * 8 + j0, t, 4);
             }
         }
     } else {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int64_t at = (static_cast<int64_t>(s) * W * 64 + lane) * 8, left = f.cols - at;
-            float *to = f.partial + blockIdx.x * static_cast<int64_t>(2) * f.cols + at;
-            if (left > 0) {
-                store_row(to, left, pack<float>(dw[s]));
-                store_row(to + f.cols, left, pack<float>(db[s]));
-            }
+            put(0, place(s), dw[s], 8);
+            put(1, place(s), db[s], 8);
         }
     }
 }
@@ -306,32 +366,46 @@ __global__ __launch_bounds__(1024) void k_layernorm_join(const float *partial, i
     *to = accumulate != 0 ? *to + t : t;
 }
 
-// Wavefronts to a row and octets per lane that hold a row: f is called with W and S as types.  Two octets per lane leave room in the registers for the row
-// behind and the weight's gradient.
+// Lanes to a row and octets per lane that hold a row: f is called with L and S as types.
 template <int N> using Int = std::integral_constant<int, N>;
 template <typename F> void with_shape(int64_t cols, F &&f) {
-    if (cols <= 512) return f(Int<1>(), Int<1>());
-    if (cols <= 1024) return f(Int<1>(), Int<2>());
-    if (cols <= 2048) return f(Int<2>(), Int<2>());
-    if (cols <= 4096) return f(Int<4>(), Int<2>());
-    if (cols <= 8192) return f(Int<8>(), Int<2>());
-    if (cols <= 16384) return f(Int<16>(), Int<2>());
-    return f(Int<16>(), Int<4>());
+    if (cols <= 64) return f(Int<8>(), Int<1>());
+    if (cols <= 128) return f(Int<16>(), Int<1>());
+    if (cols <= 256) return f(Int<32>(), Int<1>());
+    if (cols <= 512) return f(Int<64>(), Int<1>());
+    if (cols <= 1024) return f(Int<64>(), Int<2>());
+    if (cols <= 2048) return f(Int<128>(), Int<2>());
+    if (cols <= 4096) return f(Int<256>(), Int<2>());
+    if (cols <= 8192) return f(Int<512>(), Int<2>());
+    if (cols <= 16384) return f(Int<512>(), Int<4>());
+    return f(Int<1024>(), Int<4>());
 }
 
-// Wavefronts and workgroups of a launch: as many rows to a workgroup as it has teams for, but fewer where that would leave compute units without one.
+// Threads and workgroups of a launch: as many rows to a workgroup as it has teams for, but fewer where that would leave compute units without one.
 struct Launch {
-    int waves, groups;
+    int threads, groups;
 };
-Launch launch_of(int64_t rows, int waves_per_row, int groups_per_unit) {
-    int teams = waves_per_row < WAVES ? WAVES / waves_per_row : 1;
-    while (teams > 1 && rows < static_cast<int64_t>(COMPUTE_UNITS) * teams) teams /= 2;
+Launch launch_of(int64_t rows, int lanes, int groups_per_unit) {
+    int threads = threads_of(lanes);
+    while (threads > lanes && threads > 64 && rows * lanes < static_cast<int64_t>(COMPUTE_UNITS) * threads) threads /= 2;
+    const int teams = threads / lanes;
     const int64_t groups = (rows + teams - 1) / teams, most = static_cast<int64_t>(COMPUTE_UNITS) * groups_per_unit;
-    return Launch{teams * waves_per_row, static_cast<int>(groups < most ? groups : most)};
+    return Launch{threads, static_cast<int>(groups < most ? groups : most)};
 }
-// Of the backward pass: as many partial sums as workgroups.
-Launch backward_launch(int64_t rows, int waves_per_row) { return launch_of(rows, waves_per_row, 1); }
-int64_t parts_at_most(int64_t rows) { return rows < COMPUTE_UNITS ? rows : COMPUTE_UNITS; }
+// Of the backward pass: as many partial sums as workgroups.  Up to two rounds of rows are one workgroup's, which needs no join (3.5 us).  Narrow rows leave
+// registers for two workgroups to a compute unit.
+constexpr int64_t NARROW = 512;
+Launch backward_launch(int64_t rows, int lanes, int64_t cols) {
+    if (rows <= 2 * (threads_of(lanes) / lanes)) {
+        const int64_t threads = (rows * lanes + 63) / 64 * 64;
+        return Launch{static_cast<int>(threads < lanes ? lanes : threads < threads_of(lanes) ? threads : threads_of(lanes)), 1};
+    }
+    return launch_of(rows, lanes, cols <= NARROW ? 2 : 1);
+}
+int64_t parts_at_most(int64_t rows, int64_t cols) {
+    const int64_t most = cols <= NARROW ? 2 * COMPUTE_UNITS : COMPUTE_UNITS;
+    return rows < most ? rows : most;
+}
 
 bool weights_ok(const void *p, adatopk_dtype wdt) { return pointer_ok_or_null(p, static_cast<size_t>(elem_size(wdt))); }
 
@@ -353,10 +427,10 @@ adatopk_status adatopk_layernorm_forward(const void *x, int64_t x_stride, const 
                     x_stride, residual_stride, sum_stride, y_stride, rows, cols, eps,  weight_dt != dt, act8_of(act8, rows, cols)};
     with_type(dt, [&](auto *null) {
         using T = std::remove_pointer_t<decltype(null)>;
-        with_shape(cols, [&](auto waves, auto slots) {
-            constexpr int W = decltype(waves)::value, S = decltype(slots)::value;
-            const Launch l = launch_of(rows, W, 2);
-            hipLaunchKernelGGL((k_layernorm_forward<T, W, S>), dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.waves * 64)), 0,
+        with_shape(cols, [&](auto lanes, auto slots) {
+            constexpr int L = decltype(lanes)::value, S = decltype(slots)::value;
+            const Launch l = launch_of(rows, L, S == 1 ? 4 : 2);
+            hipLaunchKernelGGL((k_layernorm_forward<T, L, S>), dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.threads)), 0,
                                static_cast<hipStream_t>(hip_stream), f);
         });
     });
@@ -365,7 +439,7 @@ adatopk_status adatopk_layernorm_forward(const void *x, int64_t x_stride, const 
 
 size_t adatopk_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols) {
     if (!shape_ok(rows, cols) || cols > MAX_COLS) return 0;
-    return align_up(static_cast<size_t>(parts_at_most(rows)) * 2 * static_cast<size_t>(cols) * sizeof(float), 256);
+    return align_up(static_cast<size_t>(parts_at_most(rows, cols)) * 2 * static_cast<size_t>(cols) * sizeof(float), 256);
 }
 
 adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *act8, const float *mean,
@@ -387,19 +461,19 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
     float *partial = weights ? static_cast<float *>(workspace) : nullptr;
     if (rows > 0) {
         const Backward f{dy,        x,        weight,      dsum,      mean, rstd, dx,
-                         partial,   dy_stride, x_stride,   dsum_stride, dx_stride, rows, cols, weight_dt != dt, act8_of(const_cast<void *>(act8), rows, cols)};
+                         partial,   dweight, dbias, accumulate, dy_stride, x_stride,   dsum_stride, dx_stride, rows, cols, weight_dt != dt, act8_of(const_cast<void *>(act8), rows, cols)};
         with_type(dt, [&](auto *null) {
             using T = std::remove_pointer_t<decltype(null)>;
-            with_shape(cols, [&](auto waves, auto slots) {
-                constexpr int W = decltype(waves)::value, S = decltype(slots)::value;
-                const Launch l = backward_launch(rows, W);
+            with_shape(cols, [&](auto lanes, auto slots) {
+                constexpr int L = decltype(lanes)::value, S = decltype(slots)::value;
+                const Launch l = backward_launch(rows, L, cols);
                 parts = l.groups;
-                const auto kernel = act8 != nullptr ? k_layernorm_backward<T, W, S, true> : k_layernorm_backward<T, W, S, false>;
-                hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.waves * 64)), 0, st, f);
+                const auto kernel = act8 != nullptr ? k_layernorm_backward<T, L, S, true> : k_layernorm_backward<T, L, S, false>;
+                hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.threads)), 0, st, f);
             });
         });
     }
-    if (weights)  // (no rows: the sums are zero)
+    if (weights && parts != 1)  // (no rows: the sums are zero)
         hipLaunchKernelGGL(k_layernorm_join, dim3(static_cast<unsigned>((2 * cols + 31) / 32)), dim3(1024), 0, st, partial, parts, cols,
                            dweight, dbias, accumulate);
     return launched();

@@ -89,24 +89,78 @@ template <typename T> __device__ __forceinline__ Raw<T> load_octet(const T *p) {
     }
     return r;
 }
-template <typename T> __device__ __forceinline__ Raw<T> load_some(const T *p, int n) {  // elements [0, n), n < 8; zeros behind them
+typedef uint32_t U2a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t U2a4 __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t U1a2 __attribute__((aligned(2)));
+// Elements [0, n), 0 < n < 8, zeros behind them: four, two and one at a time.
+template <typename T> __device__ __forceinline__ Raw<T> load_some(const T *p, int n) {
     uint32_t d[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const bool four = (n & 4) != 0;
     Raw<T> r;
+    if constexpr (sizeof(T) == 4) {
+        if (four) {
+            const U4 v = *reinterpret_cast<const U4a4 *>(p);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if constexpr (sizeof(T) == 4) {
-            if (j < n) d[j] = reinterpret_cast<const uint32_t *>(p)[j];
-        } else {
-            if (j < n) d[j / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[j]) << (16 * (j % 2));
+            for (int j = 0; j < 4; ++j) d[j] = v[j];
+        }
+        if ((n & 2) != 0) {
+            const U2 v = *reinterpret_cast<const U2a4 *>(p + (n & 4));
+            d[four ? 4 : 0] = v[0];
+            d[four ? 5 : 1] = v[1];
+        }
+        if ((n & 1) != 0) {
+            const uint32_t v = reinterpret_cast<const uint32_t *>(p)[n & 6];
+#pragma unroll
+            for (int j = 0; j < 8; j += 2)
+                if ((n & 6) == j) d[j] = v;
+        }
+        r.w[1] = U4{d[4], d[5], d[6], d[7]};
+    } else {
+        if (four) {
+            const U2 v = *reinterpret_cast<const U2a2 *>(p);
+            d[0] = v[0];
+            d[1] = v[1];
+        }
+        if ((n & 2) != 0) d[four ? 2 : 0] = *reinterpret_cast<const U1a2 *>(p + (n & 4));
+        if ((n & 1) != 0) {
+            const uint32_t v = reinterpret_cast<const uint16_t *>(p)[n & 6];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if ((n & 6) == 2 * j) d[j] = v;
         }
     }
     r.w[0] = U4{d[0], d[1], d[2], d[3]};
-    if constexpr (sizeof(T) == 4) r.w[1] = U4{d[4], d[5], d[6], d[7]};
     return r;
 }
-// Octet of a row of which `left` elements follow from p on (none: zeros).
-template <typename T> __device__ __forceinline__ Raw<T> load_row(const T *p, int64_t left) {
-    if (left >= 8) return load_octet(p);
+// An octet without its first m elements, 0 < m < 8, zeros behind the rest.
+template <typename T> __device__ __forceinline__ Raw<T> without_first(const Raw<T> &r, int m) {
+    constexpr int N = sizeof(T) == 4 ? 8 : 4;  // dwords
+    uint32_t d[N + 4] = {};
+#pragma unroll
+    for (int j = 0; j < N; ++j) d[j] = r.w[j / 4][j % 4];
+    const int words = sizeof(T) == 4 ? m : m / 2;
+#pragma unroll
+    for (int step = N / 2; step > 0; step /= 2)
+#pragma unroll
+        for (int j = 0; j < N; ++j) d[j] = (words & step) != 0 ? (j + step < N ? d[j + step] : 0u) : d[j];
+    if constexpr (sizeof(T) == 2) {
+        if ((m & 1) != 0)
+#pragma unroll
+            for (int j = 0; j < N; ++j) d[j] = d[j] >> 16 | d[j + 1] << 16;
+    }
+    Raw<T> out;
+#pragma unroll
+    for (int j = 0; j < N; ++j) out.w[j / 4][j % 4] = d[j];
+    return out;
+}
+// Octet of a row of which `left` elements follow from p on (none: zeros).  A row's last octet, where it is not a whole one, is read along with what stands
+// before it (`before`: the row has eight elements before p + left), so that all lanes go the same way.
+template <typename T> __device__ __forceinline__ Raw<T> load_row(const T *p, int64_t left, bool before) {
+    if (left > 0 && (left >= 8 || before)) {
+        const int missing = left >= 8 ? 0 : 8 - static_cast<int>(left);
+        const Raw<T> r = load_octet(p - missing);
+        return missing == 0 ? r : without_first(r, missing);
+    }
     if (left > 0) return load_some(p, static_cast<int>(left));
     return Raw<T>{};
 }
@@ -143,6 +197,7 @@ template <typename T> __device__ __forceinline__ Raw<T> pack(const float (&v)[8]
     }
     return r;
 }
+// The first `left` of an octet's elements (all of them, or none).
 template <typename T> __device__ __forceinline__ void store_row(T *p, int64_t left, const Raw<T> &r) {
     if (left >= 8) {
         if constexpr (sizeof(T) == 4) {
@@ -153,13 +208,22 @@ template <typename T> __device__ __forceinline__ void store_row(T *p, int64_t le
         }
         return;
     }
-#pragma unroll
-    for (int j = 0; j < 7; ++j) {
-        if (j < left) {
-            if constexpr (sizeof(T) == 4)
-                reinterpret_cast<uint32_t *>(p)[j] = r.w[j / 4][j % 4];
-            else
-                reinterpret_cast<uint16_t *>(p)[j] = static_cast<uint16_t>(r.w[0][j / 2] >> (16 * (j % 2)));
+    if (left <= 0) return;
+    const int n = static_cast<int>(left);
+    const bool four = (n & 4) != 0;
+    if constexpr (sizeof(T) == 4) {
+        if (four) *reinterpret_cast<U4a4 *>(p) = r.w[0];
+        if ((n & 2) != 0) *reinterpret_cast<U2a4 *>(p + (n & 4)) = four ? U2{r.w[1][0], r.w[1][1]} : U2{r.w[0][0], r.w[0][1]};
+        if ((n & 1) != 0) {
+            const uint32_t low = (n & 2) != 0 ? r.w[0][2] : r.w[0][0], high = (n & 2) != 0 ? r.w[1][2] : r.w[1][0];
+            reinterpret_cast<uint32_t *>(p)[n & 6] = four ? high : low;
+        }
+    } else {
+        if (four) *reinterpret_cast<U2a2 *>(p) = U2{r.w[0][0], r.w[0][1]};
+        if ((n & 2) != 0) *reinterpret_cast<U1a2 *>(p + (n & 4)) = four ? r.w[0][2] : r.w[0][0];
+        if ((n & 1) != 0) {
+            const uint32_t low = (n & 2) != 0 ? r.w[0][1] : r.w[0][0], high = (n & 2) != 0 ? r.w[0][3] : r.w[0][2];
+            reinterpret_cast<uint16_t *>(p)[n & 6] = static_cast<uint16_t>(four ? high : low);
         }
     }
 }

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(WM *WN * 64, PER_CU * WM * WN / 4) void k_weight_gr
             for (int i = 0; i < A_OCTETS; ++i) {
                 if (i % parts != which) continue;
                 const int64_t r = row + a_row + i * A_ROWS, c = out0 + a_col;
-                ra[set][i] = load_row(static_cast<const T *>(f.dy) + r * f.dy_stride + c, r < row_end ? f.n_out - c : 0);
+                ra[set][i] = load_row(static_cast<const T *>(f.dy) + r * f.dy_stride + c, r < row_end ? f.n_out - c : 0, c > 0);
             }
         }
     };
