@@ -15,36 +15,51 @@ constexpr int NT = 256;  // threads per workgroup
 // (0, 1], where r = t * (polynomial of degree 8 in t) to 2e-8 of its value (a minimax fit in relative error).  So both tails keep their
 // relative precision.  The square's rounding would cost a^2 / 2 units in the exponential; its low part is put back to first order.
 struct Erf {
-    // Phi(x), and the density's exponential exp(-x^2 / 2)
-    static __device__ __forceinline__ float phi(float x, float &expo) {
+    // Phi(x), and the density's exponential exp(-x^2 / 2).  COARSE: for results that are rounded to 16 bits, degree 6 (1e-6) and the exponential as it
+    // comes (7e-6 where it is 1e-38, less the larger it is).
+    template <bool COARSE> static __device__ __forceinline__ float phi(float x, float &expo) {
         const float a = __builtin_fabsf(x);
-        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(a, 0.21f, 1.f));
-        float r = -0.0712955f;
-        r = __builtin_fmaf(r, t, 0.28180775f);
-        r = __builtin_fmaf(r, t, -0.32649943f);
-        r = __builtin_fmaf(r, t, 0.3449933f);
-        r = __builtin_fmaf(r, t, -0.09077693f);
-        r = __builtin_fmaf(r, t, 0.12347385f);
-        r = __builtin_fmaf(r, t, 0.06956933f);
-        r = __builtin_fmaf(r, t, 0.085012496f);
-        r = __builtin_fmaf(r, t, 0.08371515f);
-        r *= t;
         constexpr float C = -0.72134752044448170f;  // -log2(e) / 2, and what its rounding left off
         constexpr float C_LOW = static_cast<float>(-0.72134752044448170368 - static_cast<double>(C));
         const float h = x * x, k = h * C;
-        const float low = __builtin_fmaf(__builtin_fmaf(x, x, -h), C, __builtin_fmaf(h, C_LOW, __builtin_fmaf(h, C, -k)));
         const float e = __builtin_amdgcn_exp2f(k);
-        expo = k < -126.f ? 0.f : __builtin_fmaf(e, low * 0.69314718f, e);  // (also where x is infinite, and low no number)
+        float r;
+        if constexpr (COARSE) {
+            const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(a, 0.36f, 1.f));
+            r = 0.046782427f;
+            r = __builtin_fmaf(r, t, -0.17882647f);
+            r = __builtin_fmaf(r, t, 0.17967755f);
+            r = __builtin_fmaf(r, t, 0.027426654f);
+            r = __builtin_fmaf(r, t, 0.13940007f);
+            r = __builtin_fmaf(r, t, 0.14183038f);
+            r = __builtin_fmaf(r, t, 0.14370897f);
+            r *= t;
+            expo = e;
+        } else {
+            const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(a, 0.21f, 1.f));
+            r = -0.0712955f;
+            r = __builtin_fmaf(r, t, 0.28180775f);
+            r = __builtin_fmaf(r, t, -0.32649943f);
+            r = __builtin_fmaf(r, t, 0.3449933f);
+            r = __builtin_fmaf(r, t, -0.09077693f);
+            r = __builtin_fmaf(r, t, 0.12347385f);
+            r = __builtin_fmaf(r, t, 0.06956933f);
+            r = __builtin_fmaf(r, t, 0.085012496f);
+            r = __builtin_fmaf(r, t, 0.08371515f);
+            r *= t;
+            const float low = __builtin_fmaf(__builtin_fmaf(x, x, -h), C, __builtin_fmaf(h, C_LOW, __builtin_fmaf(h, C, -k)));
+            expo = k < -126.f ? 0.f : __builtin_fmaf(e, low * 0.69314718f, e);  // (also where x is infinite, and low no number)
+        }
         const float q = r * expo;
         return x < 0.f ? q : 1.f - q;
     }
     static __device__ __forceinline__ float value(float x) {
         float e;
-        return x * phi(x, e);
+        return x * phi<false>(x, e);
     }
-    static __device__ __forceinline__ float slope(float x) {  // Phi(x) + x * exp(-x^2 / 2) / sqrt(2 pi)
+    template <bool COARSE> static __device__ __forceinline__ float slope(float x) {  // Phi(x) + x * exp(-x^2 / 2) / sqrt(2 pi)
         float e;
-        const float p = phi(x, e);
+        const float p = phi<COARSE>(x, e);
         return __builtin_fmaf(x * e, 0.39894228f, p);
     }
 };
@@ -56,7 +71,7 @@ struct Tanh {
         return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(w));
     }
     static __device__ __forceinline__ float value(float x) { return x * sigmoid(x); }
-    static __device__ __forceinline__ float slope(float x) {  // s + x s (1 - s) 2 u'
+    template <bool> static __device__ __forceinline__ float slope(float x) {  // s + x s (1 - s) 2 u'
         constexpr float A = 1.5957691f, B = 0.21406445f;  // 2 sqrt(2 / pi), and that times 3 * 0.044715
         const float s = sigmoid(x), rise = x * __builtin_fmaf(x * x, B, A);
         const float d = s * (1.f - s);
@@ -125,7 +140,7 @@ __global__ __launch_bounds__(NT) void k_gelu_backward(const T *dy, int64_t dy_st
     unpack(load_row(dy + row * dy_stride + at, left, at > 0), g);
     values_of(d, E, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] *= F::slope(v[j]);
+    for (int j = 0; j < 8; ++j) g[j] *= F::template slope<sizeof(T) == 2>(v[j]);
     store_row(dx + row * dx_stride + at, left, pack<T>(g));
 }
 

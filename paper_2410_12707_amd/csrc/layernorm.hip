@@ -11,6 +11,9 @@
 
 #include "stage_ops.h"
 
+// Products and sums are fused where the code says so and nowhere else: the forms of the backward pass give the same bits.
+#pragma clang fp contract(off)
+
 namespace {
 
 using namespace adatopk_stage;
@@ -99,8 +102,8 @@ template <typename T, int L, int S> __global__ __launch_bounds__(threads_of(L)) 
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const int64_t at = place(s), left = of < f.rows ? f.cols - at : 0;
-            x[s] = load_row(static_cast<const T *>(f.x) + of * f.x_stride + at, left, at > 0);
-            if (f.residual != nullptr) r[s] = load_row(static_cast<const T *>(f.residual) + of * f.residual_stride + at, left, at > 0);
+            x[s] = fetch_row(static_cast<const T *>(f.x) + of * f.x_stride + at, left, at > 0);
+            if (f.residual != nullptr) r[s] = fetch_row(static_cast<const T *>(f.residual) + of * f.residual_stride + at, left, at > 0);
         }
     };
     float w[HELD ? S : 1][8], b[HELD ? S : 1][8];
@@ -121,10 +124,10 @@ template <typename T, int L, int S> __global__ __launch_bounds__(threads_of(L)) 
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const int64_t at = place(s), left = there ? f.cols - at : 0;
-            unpack(x[s], v[s]);
+            unpack(settle(x[s], left, at > 0), v[s]);
             if (f.residual != nullptr) {
                 float t[8];
-                unpack(r[s], t);
+                unpack(settle(r[s], left, at > 0), t);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[s][j] += t[j];
                 const Raw<T> out = pack<T>(v[s]);
@@ -176,20 +179,95 @@ struct Backward {
     float *partial;  // [parts][2][cols]: sums of dy * h and of dy over the rows of a workgroup; or, from the only workgroup, nothing
     float *dweight, *dbias;
     int accumulate;
+    int strips, row_groups;  // workgroups on columns, and behind them those on rows
     int64_t dy_stride, x_stride, dsum_stride, dx_stride;
     int64_t rows, cols;
     bool wide_weight;
     Act8 act8;
 };
 
+// Few rows: workgroups of their own add up the weight's gradient, 32 columns each, from operands that the others read at the same time.  A second read
+// of what the caches hold instead of a second launch for the partial sums.
+constexpr int STRIP = 32;
+template <typename T, bool KEEP> __device__ __forceinline__ void column_sums(const Backward &f, int strip, float *share) {
+    constexpr int AT_ONCE = 4;  // rows that a lane has on their way
+    const int octet = threadIdx.x % (STRIP / 8), first = threadIdx.x / (STRIP / 8), step = blockDim.x / (STRIP / 8);
+    const int64_t at = static_cast<int64_t>(strip) * STRIP + octet * 8, left = f.cols - at;
+    float sums[2][8] = {};
+    for (int64_t base = first; base < f.rows; base += static_cast<int64_t>(step) * AT_ONCE) {
+        Raw<T> dy[AT_ONCE], x[KEEP ? 1 : AT_ONCE];
+        U2 q[KEEP ? AT_ONCE : 1];
+        uint32_t e[KEEP ? AT_ONCE : 1];
+        float mean[AT_ONCE], rstd[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int64_t row = base + static_cast<int64_t>(i) * step, n = row < f.rows ? left : 0;
+            dy[i] = fetch_row(static_cast<const T *>(f.dy) + row * f.dy_stride + at, n, at > 0);
+            if constexpr (KEEP) {
+                q[i] = U2{0, 0};
+                e[i] = 7;
+                if (n > 0) act8_get(f.act8, row, static_cast<int>(at / 8), q[i], e[i]);
+            } else {
+                x[i] = fetch_row(static_cast<const T *>(f.x) + row * f.x_stride + at, n, at > 0);
+                mean[i] = n > 0 ? f.mean[row] : 0.f;
+                rstd[i] = n > 0 ? f.rstd[row] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int64_t n = base + static_cast<int64_t>(i) * step < f.rows ? left : 0;
+            float g[8], h[8];
+            unpack(settle(dy[i], n, at > 0), g);
+            if constexpr (KEEP) {
+                values_of(q[i], e[i], h);
+            } else {
+                unpack(settle(x[i], n, at > 0), h);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] = (h[j] - mean[i]) * rstd[i];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sums[0][j] = __builtin_fmaf(g[j], h[j], sums[0][j]);
+                sums[1][j] += g[j];
+            }
+        }
+    }
+    // the lanes' sums of a column, in a fixed order: a share of them each, then the shares
+    constexpr int VALUES = 2 * STRIP;
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) share[first * VALUES + which * STRIP + octet * 8 + j] = sums[which][j];
+    __syncthreads();
+    const int shares = blockDim.x / VALUES, value = threadIdx.x % VALUES, mine = threadIdx.x / VALUES;
+    float t = 0.f;
+    for (int k = mine; k < step; k += shares) t += share[k * VALUES + value];
+    __syncthreads();
+    share[mine * VALUES + value] = t;
+    __syncthreads();
+    if (threadIdx.x >= VALUES) return;
+    t = 0.f;
+    for (int k = 0; k < shares; ++k) t += share[k * VALUES + threadIdx.x];
+    const int64_t col = static_cast<int64_t>(strip) * STRIP + threadIdx.x % STRIP;
+    float *to = threadIdx.x < STRIP ? f.dweight : f.dbias;
+    if (to != nullptr && col < f.cols) to[col] = t + (f.accumulate != 0 ? to[col] : 0.f);
+}
+
 // Rows come round as in the forward pass.  A row's operands stay as they were loaded and are taken apart twice, for the sums and for dx: half the
 // registers of keeping them as floats, which the next row's operands take.  KEEP: h comes from the 8-bit rows.
-template <typename T, int L, int S, bool KEEP> __global__ __launch_bounds__(threads_of(L)) void k_layernorm_backward(Backward f) {
+// COLUMNS: the weight's gradient is not added up along with the rows, but, where it is asked for, by workgroups before those of the rows.
+template <typename T, int L, int S, bool KEEP, bool COLUMNS> __global__ __launch_bounds__(threads_of(L)) void k_layernorm_backward(Backward f) {
     constexpr bool HELD = held(S);
     constexpr int R = HELD ? S : 1;  // octets that are held at a time
     __shared__ float scratch[threads_of(L) / L][L > 64 ? 2 * (L / 64) : 1];
+    if constexpr (COLUMNS) {
+        if (static_cast<int>(blockIdx.x) < f.strips) {
+            __shared__ float columns[threads_of(L) * 16];
+            return column_sums<T, KEEP>(f, static_cast<int>(blockIdx.x), columns);
+        }
+    }
     const int lane = threadIdx.x % L, team = threadIdx.x / L;
-    const int64_t teams = blockDim.x / L, step = gridDim.x * teams;
+    const int64_t teams = blockDim.x / L, step = f.row_groups * teams;
     const float inverse = 1.f / static_cast<float>(f.cols);
     auto place = [&](int s) {  // (rows that are not held: what is derived from it is not kept from row to row either)
         int l = lane;
@@ -208,7 +286,7 @@ template <typename T, int L, int S, bool KEEP> __global__ __launch_bounds__(thre
     };
     auto fetch = [&](Row &to, int64_t row, int s, int at_slot, bool sum) {
         const int64_t at = place(s), left = row < f.rows ? f.cols - at : 0;
-        to.dy[at_slot] = load_row(static_cast<const T *>(f.dy) + row * f.dy_stride + at, left, at > 0);
+        to.dy[at_slot] = fetch_row(static_cast<const T *>(f.dy) + row * f.dy_stride + at, left, at > 0);
         if constexpr (KEEP) {
             if (left > 0) {
                 act8_get(f.act8, row, static_cast<int>(at / 8), to.q[at_slot], to.e[at_slot]);
@@ -217,9 +295,9 @@ template <typename T, int L, int S, bool KEEP> __global__ __launch_bounds__(thre
                 to.e[at_slot] = 7;
             }
         } else {
-            to.x[at_slot] = load_row(static_cast<const T *>(f.x) + row * f.x_stride + at, left, at > 0);
+            to.x[at_slot] = fetch_row(static_cast<const T *>(f.x) + row * f.x_stride + at, left, at > 0);
         }
-        if (sum && f.dsum != nullptr) to.ds[at_slot] = load_row(static_cast<const T *>(f.dsum) + row * f.dsum_stride + at, left, at > 0);
+        if (sum && f.dsum != nullptr) to.ds[at_slot] = fetch_row(static_cast<const T *>(f.dsum) + row * f.dsum_stride + at, left, at > 0);
     };
     auto fetch_all = [&](Row &to, int64_t row) {
         scalars(to, row);
@@ -228,24 +306,24 @@ template <typename T, int L, int S, bool KEEP> __global__ __launch_bounds__(thre
     };
     float dw[S][8] = {}, db[S][8] = {}, w[R][8];
     auto weights = [&](int s, int to) { load_weight<T>(f.weight, f.wide_weight, place(s), f.cols - place(s), 1.f, w[to]); };
-    int64_t row = blockIdx.x * teams + team;
+    const int group = static_cast<int>(blockIdx.x) - f.strips;
+    int64_t row = group * teams + team;
     Row now;
     if constexpr (HELD) {
         fetch_all(now, row);
 #pragma unroll
         for (int s = 0; s < S; ++s) weights(s, s);
     }
-    auto take = [&](const Row &from, int s, int slot, float (&g)[8], float (&h)[8]) {
-        unpack(from.dy[slot], g);
+    auto take = [&](const Row &from, int s, int slot, int64_t left, float (&g)[8], float (&h)[8]) {
+        unpack(settle(from.dy[slot], left, place(s) > 0), g);
         if constexpr (KEEP) {
             values_of(from.q[slot], from.e[slot], h);
         } else {
-            unpack(from.x[slot], h);
+            unpack(settle(from.x[slot], left, place(s) > 0), h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = (h[j] - from.mean) * from.rstd;
         }
         // (what lies behind the row is no value: without x there it would count as -mean, and a group that is marked as no number is so in its padding)
-        const int64_t left = f.cols - place(s);
         if (left < 8)
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = j < left ? h[j] : 0.f;
@@ -265,11 +343,13 @@ template <typename T, int L, int S, bool KEEP> __global__ __launch_bounds__(thre
                 weights(s, 0);
             }
             float g[8], h[8];
-            take(now, s, k, g, h);
+            take(now, s, k, row < f.rows ? f.cols - place(s) : 0, g, h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                dw[s][j] = __builtin_fmaf(g[j], h[j], dw[s][j]);
-                db[s][j] += g[j];
+                if constexpr (!COLUMNS) {
+                    dw[s][j] = __builtin_fmaf(g[j], h[j], dw[s][j]);
+                    db[s][j] += g[j];
+                }
                 g[j] *= w[k][j];
                 sums[0] += g[j];
                 sums[1] = __builtin_fmaf(g[j], h[j], sums[1]);
@@ -286,20 +366,20 @@ template <typename T, int L, int S, bool KEEP> __global__ __launch_bounds__(thre
             }
             const int64_t at = place(s), left = row < f.rows ? f.cols - at : 0;
             float g[8], h[8], add[8] = {};
-            take(now, s, k, g, h);
-            if (f.dsum != nullptr) unpack(now.ds[k], add);
+            take(now, s, k, left, g, h);
+            if (f.dsum != nullptr) unpack(settle(now.ds[k], left, at > 0), add);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) add[j] += now.rstd * (g[j] * w[k][j] - level - h[j] * along);
+            for (int j = 0; j < 8; ++j) add[j] = __builtin_fmaf(now.rstd, __builtin_fmaf(-h[j], along, __builtin_fmaf(g[j], w[k][j], -level)), add[j]);
             store_row(static_cast<T *>(f.dx) + row * f.dx_stride + at, left, pack<T>(add));
         }
         if constexpr (HELD) now = next;
     }
-    if (f.dweight == nullptr && f.dbias == nullptr) return;
+    if constexpr (COLUMNS) return;
     // n <= 8 neighbouring columns' sums: to the workgroup's place, or where there is but one, to where they belong
     auto put = [&](int which, int64_t col, const float *t, int n) {
         typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
-        const bool only = gridDim.x == 1;
-        float *to = only ? (which == 0 ? f.dweight : f.dbias) : f.partial + (blockIdx.x * static_cast<int64_t>(2) + which) * f.cols;
+        const bool only = f.row_groups == 1;
+        float *to = only ? (which == 0 ? f.dweight : f.dbias) : f.partial + (group * static_cast<int64_t>(2) + which) * f.cols;
         if (to == nullptr) return;
         to += col;
         const bool add = only && f.accumulate != 0;
@@ -402,6 +482,17 @@ Launch backward_launch(int64_t rows, int lanes, int64_t cols) {
     }
     return launch_of(rows, lanes, cols <= NARROW ? 2 : 1);
 }
+// Of the form with columns apart: whole workgroups, which the columns need, and one to a compute unit, the columns' among them.
+Launch columns_launch(int64_t rows, int lanes, int64_t cols) {
+    const int threads = threads_of(lanes), teams = threads / lanes;
+    const int64_t groups = (rows + teams - 1) / teams, strips = (cols + STRIP - 1) / STRIP;
+    const int64_t most = strips < COMPUTE_UNITS / 2 ? COMPUTE_UNITS - strips : COMPUTE_UNITS / 2;
+    return Launch{threads, static_cast<int>(groups < most ? groups : most)};
+}
+// Either form, us, columns apart / along with the rows and a second launch: 32 x 768 3.6 / 8.2, 512 x 768 fp32 4.6 / 8.8, 1000 x 1600 bf16 6.4 / 10.7, 1000 x 64 5.4 /
+// 7.8, 1000 x 4096 11.6 / 14.7, 512 x 8192 16.1 / 18.4; but 2048 x 1024 8.8 / 9.4, 2048 x 300 12.0 / 7.9, 4096 x 1024 22 / 11, 1024 x 16384 71 / 42: a strip's workgroup
+// goes through all rows, and many strips wait for one another.
+bool by_columns(int64_t rows, int64_t cols) { return rows <= 4 * COMPUTE_UNITS && rows * cols <= static_cast<int64_t>(1) << 22; }
 int64_t parts_at_most(int64_t rows, int64_t cols) {
     const int64_t most = cols <= NARROW ? 2 * COMPUTE_UNITS : COMPUTE_UNITS;
     return rows < most ? rows : most;
@@ -460,16 +551,30 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
     int parts = 0;
     float *partial = weights ? static_cast<float *>(workspace) : nullptr;
     if (rows > 0) {
-        const Backward f{dy,        x,        weight,      dsum,      mean, rstd, dx,
-                         partial,   dweight, dbias, accumulate, dy_stride, x_stride,   dsum_stride, dx_stride, rows, cols, weight_dt != dt, act8_of(const_cast<void *>(act8), rows, cols)};
+        Backward f{dy,        x,        weight,      dsum,      mean, rstd, dx,
+                         partial,   dweight, dbias, accumulate, 0, 0, dy_stride, x_stride,   dsum_stride, dx_stride, rows, cols, weight_dt != dt, act8_of(const_cast<void *>(act8), rows, cols)};
         with_type(dt, [&](auto *null) {
             using T = std::remove_pointer_t<decltype(null)>;
             with_shape(cols, [&](auto lanes, auto slots) {
                 constexpr int L = decltype(lanes)::value, S = decltype(slots)::value;
-                const Launch l = backward_launch(rows, L, cols);
-                parts = l.groups;
-                const auto kernel = act8 != nullptr ? k_layernorm_backward<T, L, S, true> : k_layernorm_backward<T, L, S, false>;
-                hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.threads)), 0, st, f);
+                const auto together = act8 != nullptr ? k_layernorm_backward<T, L, S, true, false> : k_layernorm_backward<T, L, S, false, false>;
+                const auto apart = act8 != nullptr ? k_layernorm_backward<T, L, S, true, true> : k_layernorm_backward<T, L, S, false, true>;
+                const bool columns = !weights || by_columns(rows, cols);
+                const Launch l = !columns ? backward_launch(rows, L, cols) : weights ? columns_launch(rows, L, cols) : launch_of(rows, L, 2);
+                const int strips = columns && weights ? static_cast<int>((cols + STRIP - 1) / STRIP) : 0;
+                parts = columns ? 1 : l.groups;
+                const auto launch = [&](int row_groups, int strip_groups) {
+                    f.row_groups = row_groups;
+                    f.strips = strip_groups;
+                    hipLaunchKernelGGL(columns ? apart : together, dim3(static_cast<unsigned>(row_groups + strip_groups)), dim3(static_cast<unsigned>(l.threads)), 0,
+                                       st, f);
+                };
+                if (strips != 0 && dx == dy) {  // the columns before the rows overwrite what they read
+                    launch(0, strips);
+                    launch(l.groups, 0);
+                } else {
+                    launch(l.groups, strips);
+                }
             });
         });
     }

@@ -154,16 +154,18 @@ template <typename T> __device__ __forceinline__ Raw<T> without_first(const Raw<
     return out;
 }
 // Octet of a row of which `left` elements follow from p on (none: zeros).  A row's last octet, where it is not a whole one, is read along with what stands
-// before it (`before`: the row has eight elements before p + left), so that all lanes go the same way.
-template <typename T> __device__ __forceinline__ Raw<T> load_row(const T *p, int64_t left, bool before) {
-    if (left > 0 && (left >= 8 || before)) {
-        const int missing = left >= 8 ? 0 : 8 - static_cast<int>(left);
-        const Raw<T> r = load_octet(p - missing);
-        return missing == 0 ? r : without_first(r, missing);
-    }
+// before it (`before`: the row has eight elements before p + left), so that all lanes go the same way; settle() puts it right, apart from the load, so
+// that loads can be on their way while others are waited for.
+template <typename T> __device__ __forceinline__ Raw<T> fetch_row(const T *p, int64_t left, bool before) {
+    if (left > 0 && (left >= 8 || before)) return load_octet(left >= 8 ? p : p - (8 - left));
     if (left > 0) return load_some(p, static_cast<int>(left));
     return Raw<T>{};
 }
+template <typename T> __device__ __forceinline__ Raw<T> settle(const Raw<T> &r, int64_t left, bool before) {
+    if (left >= 8 || left <= 0 || !before) return r;
+    return without_first(r, 8 - static_cast<int>(left));
+}
+template <typename T> __device__ __forceinline__ Raw<T> load_row(const T *p, int64_t left, bool before) { return settle(fetch_row(p, left, before), left, before); }
 template <typename T> __device__ __forceinline__ void unpack(const Raw<T> &r, float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
