@@ -65,6 +65,67 @@ __device__ __forceinline__ int place(int b, int n) {
     return xcd * per + (xcd < more ? xcd : more) + b / 8;
 }
 
+// A tile's results to where they belong: the weight's gradient, or with the tokens split the partial products.  A register holds four rows' results of 32
+// columns in each half of the wavefront, so a store's address is a scalar and an offset per lane.
+template <typename T, int BM, int BN, int WM, int WN, int MI, int NI, typename Block>
+__device__ __forceinline__ void finish(const Product &f, const F16v (&acc)[MI][NI], const float *sums, Block &&block, int64_t out0, int64_t own_out, int64_t in0,
+                                       int64_t own_in, int part) {
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), wm = wave / WN, wn = wave % WN;
+    const bool last = f.split == 1;
+    if (own_in == 0) {
+        float *to = last ? f.db : f.partial_db + part * f.n_out;
+        if (to != nullptr)
+            for (int i = tid; i < BM && out0 + i < f.n_out; i += WM * WN * 64)
+                if (out0 + i >= own_out) to[out0 + i] = sums[i] + (last && f.accumulate != 0 ? to[out0 + i] : 0.f);
+    }
+    const int64_t row0 = out0 + wm * (BM / WM), col0 = in0 + wn * (BN / WN);
+    float *const to = (last ? f.dw : f.partial + part * f.n_out * f.n_in) + row0 * f.n_in + col0;
+    const uint32_t offset = static_cast<uint32_t>(4 * (lane / 32)) * static_cast<uint32_t>(f.n_in) + lane % 32;
+    const bool inside = out0 == own_out && out0 + BM <= f.n_out && in0 == own_in && in0 + BN <= f.n_in;
+    const bool plain = !last || (f.weight == nullptr && f.bias == nullptr && f.accumulate == 0);
+    if (inside && plain) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                float *const row = to + (block(i) * 32 + 8 * (q / 4) + q % 4) * f.n_in;
+#pragma unroll
+                for (int j = 0; j < NI; ++j) row[offset + j * 32] = acc[i][j][q];
+            }
+        return;
+    }
+    float w[NI], v[NI];
+    bool mine[NI];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+        const int64_t c = col0 + j * 32 + lane % 32;
+        mine[j] = c >= own_in && c < f.n_in;
+        const bool there = last && mine[j];
+        w[j] = there ? weight_at(f.weight, f.wide_weight || sizeof(T) == 4, __is_same(T, F16), c, 1.f) : 1.f;
+        v[j] = there ? weight_at(f.bias, f.wide_weight || sizeof(T) == 4, __is_same(T, F16), c, 0.f) : 0.f;
+    }
+    const bool scaled = last && f.weight != nullptr, shifted = last && f.bias != nullptr, add = last && f.accumulate != 0;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const int m = block(i) * 32 + 8 * (q / 4) + q % 4;
+            const int64_t r = row0 + m + 4 * (lane / 32);
+            if (!inside && (r >= f.n_out || r < own_out)) continue;
+            float *const row = to + m * f.n_in;
+            const float sum = shifted ? sums[wm * (BM / WM) + m + 4 * (lane / 32)] : 0.f;
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                if (!inside && !mine[j]) continue;
+                float t = acc[i][j][q];
+                if (scaled) t *= w[j];
+                if (shifted) t = __builtin_fmaf(sum, v[j], t);
+                if (add) t += row[offset + j * 32];
+                row[offset + j * 32] = t;
+            }
+        }
+}
+
 // One tile of BM x BN results over one share of the tokens, four wavefronts, a quarter of the tile each.  Tiles of BK tokens go through two buffers in
 // LDS: while the matrix instructions work on one, the next is converted into the other and the one behind it is on its way into registers.  One
 // barrier per tile, and the last step's operands are in registers when it comes, so the matrix unit has work across it.
@@ -109,7 +170,8 @@ __global__ __launch_bounds__(WM *WN * 64, PER_CU * WM * WN / 4) void k_weight_gr
     auto fetch = [&](auto within, int set, int64_t row, int which, int parts) {
         constexpr bool WITHIN = decltype(within)::value;
         typedef const __attribute__((address_space(1))) char Global;
-        if constexpr (WITHIN) {
+        if (!WITHIN && row >= row_end) return;  // (what the registers hold goes into a buffer that nobody reads)
+        if (WITHIN || (!SMALL && row + BK <= row_end)) {
             // (scalar bases that the optimiser cannot see through: an address is a base and a 32-bit offset, not a 64-bit variable of its own)
 #pragma unroll
             for (int i = 0; i < B_PIECES; ++i) {
@@ -286,36 +348,7 @@ __global__ __launch_bounds__(WM *WN * 64, PER_CU * WM * WN / 4) void k_weight_gr
         if (lane < 32 && wn * CI < MI) sums[wm * (BM / WM) + block(i) * 32 + lane] = t;
     }
     __syncthreads();
-    const bool last = f.split == 1;
-    if (own_in == 0) {
-        float *to = last ? f.db : f.partial_db + part * f.n_out;
-        if (to != nullptr)
-            for (int i = tid; i < BM && out0 + i < f.n_out; i += NT)
-                if (out0 + i >= own_out) to[out0 + i] = sums[i] + (last && f.accumulate != 0 ? to[out0 + i] : 0.f);
-    }
-    float *to = last ? f.dw : f.partial + part * f.n_out * f.n_in;
-#pragma unroll
-    for (int j = 0; j < NI; ++j) {
-        const int64_t c = in0 + wn * (BN / WN) + j * 32 + lane % 32;
-        if (c >= f.n_in || c < own_in) continue;
-        const float w = last ? weight_at(f.weight, f.wide_weight || sizeof(T) == 4, __is_same(T, F16), c, 1.f) : 1.f;
-        const float v = last ? weight_at(f.bias, f.wide_weight || sizeof(T) == 4, __is_same(T, F16), c, 0.f) : 0.f;
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const int m = wm * (BM / WM) + block(i) * 32 + 8 * (q / 4) + 4 * (lane / 32) + q % 4;
-                if (out0 + m >= f.n_out || out0 + m < own_out) continue;
-                float *at = to + (out0 + m) * f.n_in + c;
-                float t = acc[i][j][q];
-                if (last) {
-                    if (f.weight != nullptr) t *= w;
-                    if (f.bias != nullptr) t = __builtin_fmaf(sums[m], v, t);
-                    if (f.accumulate != 0) t += *at;
-                }
-                *at = t;
-            }
-    }
+    finish<T, BM, BN, WM, WN>(f, acc, sums, block, out0, own_out, in0, own_in, part);
 }
 
 // The partial products added up in the order of the tokens, weight and bias applied.  Four results per thread, wherever rows end.
@@ -393,9 +426,9 @@ struct Cut {
 // pieces of dY (bf16, fp16, fp32) and by tile; and what a workgroup takes beside its steps.  Measured over 1024 and 4096 tokens with 256 and 512
 // workgroups.  The larger tiles do two and a half times the work per time of the 64 x 64, but there are fewer of them: which tile and how many shares
 // of the tokens are best is the least of the sums below.
-constexpr float STEP_ALONE[3][TILES] = {{1.93f, 1.46f, 1.09f, 1.06f, 0.37f, 0.5f}, {3.3f, 0.f, 2.27f, 1.45f, 0.64f, 0.9f}, {4.78f, 0.f, 3.06f, 1.89f, 0.87f, 1.2f}};
-constexpr float STEP_FULL[3][TILES] = {{1.93f, 1.46f, 1.09f, 1.31f, 0.58f, 0.8f}, {3.3f, 0.f, 2.27f, 2.46f, 1.02f, 1.4f}, {4.78f, 0.f, 3.06f, 1.89f, 0.87f, 1.2f}};
-constexpr float BESIDE[TILES] = {22.f, 20.f, 14.f, 12.f, 6.f, 6.f};
+constexpr float STEP_ALONE[3][TILES] = {{1.9f, 1.45f, 1.06f, 1.07f, 0.39f, 0.5f}, {3.25f, 0.f, 2.4f, 1.6f, 0.64f, 0.9f}, {4.55f, 0.f, 2.95f, 1.9f, 0.85f, 1.2f}};
+constexpr float STEP_FULL[3][TILES] = {{1.9f, 1.45f, 1.06f, 1.31f, 0.58f, 0.8f}, {3.25f, 0.f, 2.4f, 2.46f, 1.01f, 1.4f}, {4.55f, 0.f, 2.95f, 1.9f, 0.85f, 1.2f}};
+constexpr float BESIDE[TILES] = {14.f, 13.f, 8.f, 5.f, 4.5f, 5.f};
 constexpr int SPLIT_MAX = 16;
 int per_unit(int tile, int pieces) { return tile < TILE_128_128 || pieces == 3 ? 1 : 2; }  // (fp32's tiles take the LDS of one)
 
@@ -417,7 +450,10 @@ Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, bool far
             const double alone = BESIDE[t] + static_cast<double>(STEP_ALONE[pieces - 1][t]) * per, together = BESIDE[t] + static_cast<double>(STEP_FULL[pieces - 1][t]) * per;
             // partial products written and read, and a launch: 5 us and 0.4 us for each MB of a share's
             const double join = split == 1 ? 0. : 5. + 0.4e-6 * 4. * static_cast<double>(split) * static_cast<double>(n_out * n_in);
-            const double cost = full * together + (rest == 0 ? 0. : rest <= 256 ? alone : together) + join;
+            // workgroups that share a compute unit do not end together: their rounds run into one another
+            const double rounds = per_unit(t, pieces) == 1 || full == 0 ? full * together + (rest == 0 ? 0. : rest <= 256 ? alone : together)
+                                                                        : static_cast<double>(tiles * split) / places * together;
+            const double cost = rounds + join;
             if (best.split == 0 || cost < least) {
                 least = cost;
                 best = Cut{static_cast<Tile>(t), static_cast<int>(in), static_cast<int>(tiles), static_cast<int>(split), per * SHARE};
@@ -468,7 +504,6 @@ adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void
     with_type(dt, [&](auto *null) {
         using T = std::remove_pointer_t<decltype(null)>;
         constexpr int DEEP = pieces_of<T>() == 1 ? 64 : 32;  // tokens of a tile: what two buffers have room for
-        constexpr int SHALLOW = pieces_of<T>() == 1 ? 64 : 64;
         const auto launch = [&](auto kernel, int threads) {
             hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(c.tiles * c.split)), dim3(static_cast<unsigned>(threads)), 0, st, f);
         };
@@ -481,9 +516,9 @@ adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void
         } else if (c.tile == TILE_128_128)
             launch(k_weight_grad<T, 128, 128, 32, 2, 2, pieces_of<T>() < 3 ? 2 : 1, 1, false>, 256);
         else if (c.tile == TILE_64_64)
-            launch(k_weight_grad<T, 64, 64, SHALLOW, 2, 2, pieces_of<T>() < 3 ? 2 : 1, 2, false>, 256);
+            launch(k_weight_grad<T, 64, 64, 64, 2, 2, pieces_of<T>() < 3 ? 2 : 1, 2, false>, 256);
         else
-            launch(k_weight_grad<T, 64, 64, SHALLOW, 2, 2, pieces_of<T>() < 3 ? 2 : 1, 2, true>, 256);
+            launch(k_weight_grad<T, 64, 64, 64, 2, 2, pieces_of<T>() < 3 ? 2 : 1, 2, true>, 256);
     });
     if (c.split > 1)
         hipLaunchKernelGGL(k_weight_join, dim3(static_cast<unsigned>((n_out * n_in + 1023) / 1024)), dim3(256), 0, st,
