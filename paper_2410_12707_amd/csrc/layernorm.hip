@@ -176,7 +176,7 @@ struct Backward {
     const void *dy, *x, *weight, *dsum;
     const float *mean, *rstd;
     void *dx;
-    float *partial;  // [parts][2][cols]: sums of dy * h and of dy over the rows of a workgroup; or, from the only workgroup, nothing
+    float *partial;  // [parts][2][cols]: sums of dy * h and of dy over the rows of a workgroup
     float *dweight, *dbias;
     int accumulate;
     int strips, row_groups;  // workgroups on columns, and behind them those on rows
@@ -375,24 +375,18 @@ template <typename T, int L, int S, bool KEEP, bool COLUMNS> __global__ __launch
         if constexpr (HELD) now = next;
     }
     if constexpr (COLUMNS) return;
-    // n <= 8 neighbouring columns' sums: to the workgroup's place, or where there is but one, to where they belong
+    // n <= 8 neighbouring columns' sums, to the workgroup's place
     auto put = [&](int which, int64_t col, const float *t, int n) {
         typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
-        const bool only = f.row_groups == 1;
-        float *to = only ? (which == 0 ? f.dweight : f.dbias) : f.partial + (group * static_cast<int64_t>(2) + which) * f.cols;
-        if (to == nullptr) return;
-        to += col;
-        const bool add = only && f.accumulate != 0;
+        float *to = f.partial + (group * static_cast<int64_t>(2) + which) * f.cols + col;
 #pragma unroll
         for (int j = 0; j < n; j += 4) {
             if (col + j + 4 <= f.cols) {
-                F4 v = {t[j], t[j + 1], t[j + 2], t[j + 3]};
-                if (add) v += *reinterpret_cast<const F4 *>(to + j);
-                *reinterpret_cast<F4 *>(to + j) = v;
+                *reinterpret_cast<F4 *>(to + j) = F4{t[j], t[j + 1], t[j + 2], t[j + 3]};
             } else {
 #pragma unroll
                 for (int i = 0; i < 3; ++i)
-                    if (col + j + i < f.cols) to[j + i] = t[j + i] + (add ? to[j + i] : 0.f);
+                    if (col + j + i < f.cols) to[j + i] = t[j + i];
             }
         }
     };
@@ -448,12 +442,17 @@ __global__ __launch_bounds__(1024) void k_layernorm_join(const float *partial, i
 
 // Lanes to a row and octets per lane that hold a row: f is called with L and S as types.
 template <int N> using Int = std::integral_constant<int, N>;
-template <typename F> void with_shape(int64_t cols, F &&f) {
+//
+// The backward pass takes 1025 to 2048 columns with an octet to a lane and two workgroups to a compute unit, whose loads cover one another's sums: 16384 x 1600
+// bf16 from 8-bit rows 35.5 us against 39.8 with two octets and one workgroup, from x 39.6 / 42.5, 8192 x 2048 fp32 30.5 / 32.4.  The forward pass takes two
+// octets there (21.5 / 23.6), and so does the backward pass with more columns (4096 x 4096 fp32 33.2 / 37.3, 4096 x 8192 bf16 42.0 / 47.0).
+template <bool BACKWARD, typename F> void with_shape(int64_t cols, F &&f) {
     if (cols <= 64) return f(Int<8>(), Int<1>());
     if (cols <= 128) return f(Int<16>(), Int<1>());
     if (cols <= 256) return f(Int<32>(), Int<1>());
     if (cols <= 512) return f(Int<64>(), Int<1>());
     if (cols <= 1024) return f(Int<64>(), Int<2>());
+    if (BACKWARD && cols > 1024 && cols <= 2048) return f(Int<256>(), Int<1>());
     if (cols <= 2048) return f(Int<128>(), Int<2>());
     if (cols <= 4096) return f(Int<256>(), Int<2>());
     if (cols <= 8192) return f(Int<512>(), Int<2>());
@@ -472,16 +471,8 @@ Launch launch_of(int64_t rows, int lanes, int groups_per_unit) {
     const int64_t groups = (rows + teams - 1) / teams, most = static_cast<int64_t>(COMPUTE_UNITS) * groups_per_unit;
     return Launch{threads, static_cast<int>(groups < most ? groups : most)};
 }
-// Of the backward pass: as many partial sums as workgroups.  Up to two rounds of rows are one workgroup's, which needs no join (3.5 us).  Narrow rows leave
-// registers for two workgroups to a compute unit.
-constexpr int64_t NARROW = 512;
-Launch backward_launch(int64_t rows, int lanes, int64_t cols) {
-    if (rows <= 2 * (threads_of(lanes) / lanes)) {
-        const int64_t threads = (rows * lanes + 63) / 64 * 64;
-        return Launch{static_cast<int>(threads < lanes ? lanes : threads < threads_of(lanes) ? threads : threads_of(lanes)), 1};
-    }
-    return launch_of(rows, lanes, cols <= NARROW ? 2 : 1);
-}
+// Workgroups of the backward pass to a compute unit: each writes a partial sum, and one octet to a lane leaves registers for two.
+int groups_per_unit(int slots) { return slots == 1 ? 2 : 1; }
 // Of the form with columns apart: whole workgroups, which the columns need, and one to a compute unit, the columns' among them.
 Launch columns_launch(int64_t rows, int lanes, int64_t cols) {
     const int threads = threads_of(lanes), teams = threads / lanes;
@@ -494,7 +485,8 @@ Launch columns_launch(int64_t rows, int lanes, int64_t cols) {
 // goes through all rows, and many strips wait for one another.
 bool by_columns(int64_t rows, int64_t cols) { return rows <= 4 * COMPUTE_UNITS && rows * cols <= static_cast<int64_t>(1) << 22; }
 int64_t parts_at_most(int64_t rows, int64_t cols) {
-    const int64_t most = cols <= NARROW ? 2 * COMPUTE_UNITS : COMPUTE_UNITS;
+    int64_t most = 0;
+    with_shape<true>(cols, [&](auto, auto slots) { most = static_cast<int64_t>(COMPUTE_UNITS) * groups_per_unit(slots()); });
     return rows < most ? rows : most;
 }
 
@@ -518,7 +510,7 @@ adatopk_status adatopk_layernorm_forward(const void *x, int64_t x_stride, const 
                     x_stride, residual_stride, sum_stride, y_stride, rows, cols, eps,  weight_dt != dt, act8_of(act8, rows, cols)};
     with_type(dt, [&](auto *null) {
         using T = std::remove_pointer_t<decltype(null)>;
-        with_shape(cols, [&](auto lanes, auto slots) {
+        with_shape<false>(cols, [&](auto lanes, auto slots) {
             constexpr int L = decltype(lanes)::value, S = decltype(slots)::value;
             const Launch l = launch_of(rows, L, S == 1 ? 4 : 2);
             hipLaunchKernelGGL((k_layernorm_forward<T, L, S>), dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.threads)), 0,
@@ -551,16 +543,16 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
     int parts = 0;
     float *partial = weights ? static_cast<float *>(workspace) : nullptr;
     if (rows > 0) {
-        Backward f{dy,        x,        weight,      dsum,      mean, rstd, dx,
-                         partial,   dweight, dbias, accumulate, 0, 0, dy_stride, x_stride,   dsum_stride, dx_stride, rows, cols, weight_dt != dt, act8_of(const_cast<void *>(act8), rows, cols)};
+        Backward f{dy, x, weight, dsum, mean, rstd, dx, partial, dweight, dbias, accumulate, 0, 0, dy_stride, x_stride, dsum_stride, dx_stride, rows, cols,
+                   weight_dt != dt, act8_of(const_cast<void *>(act8), rows, cols)};
         with_type(dt, [&](auto *null) {
             using T = std::remove_pointer_t<decltype(null)>;
-            with_shape(cols, [&](auto lanes, auto slots) {
+            with_shape<true>(cols, [&](auto lanes, auto slots) {
                 constexpr int L = decltype(lanes)::value, S = decltype(slots)::value;
                 const auto together = act8 != nullptr ? k_layernorm_backward<T, L, S, true, false> : k_layernorm_backward<T, L, S, false, false>;
                 const auto apart = act8 != nullptr ? k_layernorm_backward<T, L, S, true, true> : k_layernorm_backward<T, L, S, false, true>;
                 const bool columns = !weights || by_columns(rows, cols);
-                const Launch l = !columns ? backward_launch(rows, L, cols) : weights ? columns_launch(rows, L, cols) : launch_of(rows, L, 2);
+                const Launch l = !columns ? launch_of(rows, L, groups_per_unit(S)) : weights ? columns_launch(rows, L, cols) : launch_of(rows, L, 2);
                 const int strips = columns && weights ? static_cast<int>((cols + STRIP - 1) / STRIP) : 0;
                 parts = columns ? 1 : l.groups;
                 const auto launch = [&](int row_groups, int strip_groups) {
@@ -578,7 +570,7 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
             });
         });
     }
-    if (weights && parts != 1)  // (no rows: the sums are zero)
+    if (weights && parts != 1)  // (no rows: the sums are zero.  A matrix whose columns are not apart is always several workgroups')
         hipLaunchKernelGGL(k_layernorm_join, dim3(static_cast<unsigned>((2 * cols + 31) / 32)), dim3(1024), 0, st, partial, parts, cols,
                            dweight, dbias, accumulate);
     return launched();
