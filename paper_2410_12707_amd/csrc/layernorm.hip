@@ -23,21 +23,18 @@ constexpr int64_t MAX_COLS = 32768;        // 1024 lanes with four octets each
 // Threads of the largest workgroup, by the lanes to a row.
 constexpr int threads_of(int lanes) { return lanes < 512 ? 512 : lanes; }
 
-// A row is a team's: L lanes, from an eighth of a wavefront to a whole workgroup.  Sum over them, in a fixed order, in every lane; `scratch`: a float per
+// A row is a team's: L lanes, from an eighth of a wavefront to a whole workgroup.  Sum over them, in a fixed order, in every lane; `scratch`: a place per
 // wavefront and value in LDS, the team's own.  Every lane of the workgroup calls it.
-template <int CONTROL> __device__ __forceinline__ float moved(float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xF, 0xF, false));
-}
-template <int L, int N> __device__ __forceinline__ void team_sum(float (&v)[N], float *scratch) {
+template <int L, int N, typename V> __device__ __forceinline__ void team_sum(V (&v)[N], V *scratch) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if constexpr (L >= 64) {
             v[i] = wave_sum(v[i]);
         } else {
-            v[i] += moved<0xB1>(v[i]);   // the neighbour, the other pair of the quad, the other quad of eight lanes, the other half of sixteen
-            v[i] += moved<0x4E>(v[i]);
-            v[i] += moved<0x141>(v[i]);
-            if constexpr (L >= 16) v[i] += moved<0x140>(v[i]);
+            v[i] += moved<0xB1, 0xF, false>(v[i]);   // the neighbour, the other pair of the quad, the other quad of eight lanes, the other half of sixteen
+            v[i] += moved<0x4E, 0xF, false>(v[i]);
+            v[i] += moved<0x141, 0xF, false>(v[i]);
+            if constexpr (L >= 16) v[i] += moved<0x140, 0xF, false>(v[i]);
             if constexpr (L >= 32) v[i] += __shfl_xor(v[i], 16);
         }
     }
@@ -51,7 +48,7 @@ template <int L, int N> __device__ __forceinline__ void team_sum(float (&v)[N], 
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float t = 0.f;
+            V t = 0;
 #pragma unroll
             for (int w = 0; w < W; ++w) t += scratch[i * W + w];
             v[i] = t;
@@ -87,10 +84,11 @@ template <typename T> __device__ __forceinline__ void load_weight(const void *p,
 // one is summed up.
 template <typename T, int L, int S> __global__ __launch_bounds__(threads_of(L)) void k_layernorm_forward(Forward f) {
     constexpr bool HELD = held(S);
-    __shared__ float scratch[threads_of(L) / L][L > 64 ? L / 64 : 1];
+    __shared__ double scratch[threads_of(L) / L][L > 64 ? L / 64 : 1];
+    __shared__ float squares[threads_of(L) / L][L > 64 ? L / 64 : 1];
     const int lane = threadIdx.x % L, team = threadIdx.x / L;
     const int64_t teams = blockDim.x / L, step = gridDim.x * teams;
-    const float inverse = 1.f / static_cast<float>(f.cols);
+    const double inverse = 1.0 / static_cast<double>(f.cols);
     int64_t row = blockIdx.x * teams + team;
     auto place = [&](int s) {  // (rows that are not held: what is derived from it is not kept from row to row either)
         int l = lane;
@@ -120,7 +118,7 @@ template <typename T, int L, int S> __global__ __launch_bounds__(threads_of(L)) 
         const bool there = row < f.rows;
         if constexpr (!HELD) fetch(row);
         float v[S][8];
-        float sums[1] = {0.f};
+        double sums[1] = {0.0};  // (64 bits: what is left of values that cancel is the mean)
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const int64_t at = place(s), left = there ? f.cols - at : 0;
@@ -139,18 +137,18 @@ template <typename T, int L, int S> __global__ __launch_bounds__(threads_of(L)) 
         }
         if constexpr (HELD) fetch(row + step);
         team_sum<L>(sums, scratch[team]);
-        const float mean = sums[0] * inverse;
-        sums[0] = 0.f;
+        const float mean = static_cast<float>(sums[0] * inverse);
+        float square[1] = {0.f};
 #pragma unroll
         for (int s = 0; s < S; ++s) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 v[s][j] = place(s) + j < f.cols ? v[s][j] - mean : 0.f;
-                sums[0] = __builtin_fmaf(v[s][j], v[s][j], sums[0]);
+                square[0] = __builtin_fmaf(v[s][j], v[s][j], square[0]);
             }
         }
-        team_sum<L>(sums, scratch[team]);
-        const float rstd = 1.f / __fsqrt_rn(sums[0] * inverse + f.eps);
+        team_sum<L>(square, squares[team]);
+        const float rstd = 1.f / __fsqrt_rn(square[0] * static_cast<float>(inverse) + f.eps);
         if (lane == 0 && there) {
             if (f.mean != nullptr) f.mean[row] = mean;
             if (f.rstd != nullptr) f.rstd[row] = rstd;

@@ -295,19 +295,29 @@ __device__ __forceinline__ void act8_get(const Act8 &a, int64_t row, int octet, 
     }
 }
 
+// A value of another lane, zero where `rows` takes none; 64-bit ones in halves.
+template <int CONTROL, int ROWS, bool ZERO> __device__ __forceinline__ float moved(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, ROWS, 0xF, ZERO));
+}
+template <int CONTROL, int ROWS, bool ZERO> __device__ __forceinline__ double moved(double v) {
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CONTROL, ROWS, 0xF, ZERO),
+                            __builtin_amdgcn_update_dpp(0, __double2loint(v), CONTROL, ROWS, 0xF, ZERO));
+}
+__device__ __forceinline__ float from_lane(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+__device__ __forceinline__ double from_lane(double v, int lane) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+
 // Sum over the 64 lanes, in a fixed order, as a scalar.  Moves within a row of 16 lanes and from row to row ride on the additions: a tenth of the
 // latency of exchanges through LDS.
-__device__ __forceinline__ float wave_sum(float v) {
-    const auto moved = [](float x, auto control, auto rows) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(control)::value, decltype(rows)::value, 0xF, true));
-    };
-    v += moved(v, std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xF>());  // row_shr 1, 2, 4, 8: a row's last lane has its sum
-    v += moved(v, std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xF>());
-    v += moved(v, std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xF>());
-    v += moved(v, std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xF>());
-    v += moved(v, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xA>());  // row_bcast 15: into rows 1 and 3
-    v += moved(v, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xC>());  // row_bcast 31: into rows 2 and 3
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+template <typename V> __device__ __forceinline__ V wave_sum(V v) {
+    v += moved<0x111, 0xF, true>(v);  // row_shr 1, 2, 4, 8: a row's last lane has its sum
+    v += moved<0x112, 0xF, true>(v);
+    v += moved<0x114, 0xF, true>(v);
+    v += moved<0x118, 0xF, true>(v);
+    v += moved<0x142, 0xA, true>(v);  // row_bcast 15: into rows 1 and 3
+    v += moved<0x143, 0xC, true>(v);  // row_bcast 31: into rows 2 and 3
+    return from_lane(v, 63);
 }
 
 // Division of a 32-bit number by one that a launch fixes: one multiplication and a shift (Granlund and Montgomery's round-up form, n < 2^31).
