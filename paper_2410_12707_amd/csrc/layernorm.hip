@@ -132,8 +132,12 @@ template <typename T, int L, int S> __global__ __launch_bounds__(threads_of(L)) 
                 if (f.sum != nullptr) store_row(static_cast<T *>(f.sum) + row * f.sum_stride + at, left, out);
                 unpack(out, v[s]);
             }
+            if constexpr (sizeof(T) == 2) {  // (eight values of 8 or 11 bits add up in 24 but for what lies 2^10 below the largest)
+                sums[0] += ((v[s][0] + v[s][1]) + (v[s][2] + v[s][3])) + ((v[s][4] + v[s][5]) + (v[s][6] + v[s][7]));
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sums[0] += v[s][j];
+                for (int j = 0; j < 8; ++j) sums[0] += v[s][j];
+            }
         }
         if constexpr (HELD) fetch(row + step);
         team_sum<L>(sums, scratch[team]);
