@@ -126,9 +126,14 @@ __device__ __forceinline__ void finish(const Product &f, const F16v (&acc)[MI][N
         }
 }
 
-// One tile of BM x BN results over one share of the tokens, four wavefronts, a quarter of the tile each.  Tiles of BK tokens go through two buffers in
+// One tile of BM x BN results over one share of the tokens, WM x WN wavefronts, an equal part of the tile each.  Tiles of BK tokens go through two buffers in
 // LDS: while the matrix instructions work on one, the next is converted into the other and the one behind it is on its way into registers.  One
 // barrier per tile, and the last step's operands are in registers when it comes, so the matrix unit has work across it.
+//
+// 16384 tokens, 6400 x 1600, bf16 (tiles of 256 x 192): 368 us, 910 TFLOP/s.  Parts of the loop alone: the matrix instructions and the barrier 200 us, with
+// the reads from LDS 235 to 257; the rest is dY and the 8-bit numbers on their way into LDS, whose conversion and stores share the issue slots and LDS
+// with them.  512 tokens, 768 x 768, fp32 (three products): 11.5 us; 2049 tokens, 777 x 1000, fp16 (two): 29 us, both of them a few rounds of workgroups whose
+// start and end are most of it.
 //
 // The last tile of a row or column of tiles begins so far ahead that it ends with the matrix (it stores what is its own), so loads need no bounds but
 // those of the tokens.  SMALL: the matrix is narrower than the tile, or its rows too far apart for 32-bit offsets; every load is bounded.
@@ -351,7 +356,8 @@ __global__ __launch_bounds__(WM *WN * 64, PER_CU * WM * WN / 4) void k_weight_gr
     finish<T, BM, BN, WM, WN>(f, acc, sums, block, out0, own_out, in0, own_in, part);
 }
 
-// The partial products added up in the order of the tokens, weight and bias applied.  Four results per thread, wherever rows end.
+// The partial products added up in the order of the tokens, weight and bias applied.  Four results per thread, wherever rows end.  Bound by memory, and on
+// small matrices by the launch: the planner counts 5 us and 0.4 us for each MB of a share's results.
 struct Join {
     Product f;
     Divisor per_row;  // n_in
