@@ -183,6 +183,7 @@ struct Backward {
     float *dweight, *dbias;
     int accumulate;
     int strips, row_groups;  // workgroups on columns, and behind them those on rows
+    int64_t strip_rows;      // rows of a strip's workgroup; fewer than all: strips of several shares of the rows, each with a partial sum
     int64_t dy_stride, x_stride, dsum_stride, dx_stride;
     int64_t rows, cols;
     bool wide_weight;
@@ -190,21 +191,24 @@ struct Backward {
 };
 
 // Few rows: workgroups of their own add up the weight's gradient, 32 columns each, from operands that the others read at the same time.  A second read
-// of what the caches hold instead of a second launch for the partial sums.
+// of what the caches hold instead of a second launch for the partial sums.  And the widest rows, beside whose own registers the sums have no place: there the
+// rows are cut into shares.
 constexpr int STRIP = 32;
-template <typename T, bool KEEP> __device__ __forceinline__ void column_sums(const Backward &f, int strip, float *share) {
+template <typename T, bool KEEP> __device__ __forceinline__ void column_sums(const Backward &f, int group, float *share) {
     constexpr int AT_ONCE = 4;  // rows that a lane has on their way
     const int octet = threadIdx.x % (STRIP / 8), first = threadIdx.x / (STRIP / 8), step = blockDim.x / (STRIP / 8);
+    const int strips = static_cast<int>((f.cols + STRIP - 1) / STRIP), strip = group % strips, part = group / strips;
+    const int64_t begin = part * f.strip_rows, end = begin + f.strip_rows < f.rows ? begin + f.strip_rows : f.rows;
     const int64_t at = static_cast<int64_t>(strip) * STRIP + octet * 8, left = f.cols - at;
     float sums[2][8] = {};
-    for (int64_t base = first; base < f.rows; base += static_cast<int64_t>(step) * AT_ONCE) {
+    for (int64_t base = begin + first; base < end; base += static_cast<int64_t>(step) * AT_ONCE) {
         Raw<T> dy[AT_ONCE], x[KEEP ? 1 : AT_ONCE];
         U2 q[KEEP ? AT_ONCE : 1];
         uint32_t e[KEEP ? AT_ONCE : 1];
         float mean[AT_ONCE], rstd[AT_ONCE];
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-            const int64_t row = base + static_cast<int64_t>(i) * step, n = row < f.rows ? left : 0;
+            const int64_t row = base + static_cast<int64_t>(i) * step, n = row < end ? left : 0;
             dy[i] = fetch_row(static_cast<const T *>(f.dy) + row * f.dy_stride + at, n, at > 0);
             if constexpr (KEEP) {
                 q[i] = U2{0, 0};
@@ -218,7 +222,7 @@ template <typename T, bool KEEP> __device__ __forceinline__ void column_sums(con
         }
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-            const int64_t n = base + static_cast<int64_t>(i) * step < f.rows ? left : 0;
+            const int64_t n = base + static_cast<int64_t>(i) * step < end ? left : 0;
             float g[8], h[8];
             unpack(settle(dy[i], n, at > 0), g);
             if constexpr (KEEP) {
@@ -252,8 +256,9 @@ template <typename T, bool KEEP> __device__ __forceinline__ void column_sums(con
     t = 0.f;
     for (int k = 0; k < shares; ++k) t += share[k * VALUES + threadIdx.x];
     const int64_t col = static_cast<int64_t>(strip) * STRIP + threadIdx.x % STRIP;
-    float *to = threadIdx.x < STRIP ? f.dweight : f.dbias;
-    if (to != nullptr && col < f.cols) to[col] = t + (f.accumulate != 0 ? to[col] : 0.f);
+    const bool whole = f.strip_rows >= f.rows;
+    float *to = !whole ? f.partial + (part * static_cast<int64_t>(2) + (threadIdx.x < STRIP ? 0 : 1)) * f.cols : threadIdx.x < STRIP ? f.dweight : f.dbias;
+    if (to != nullptr && col < f.cols) to[col] = t + (whole && f.accumulate != 0 ? to[col] : 0.f);
 }
 
 // Rows come round as in the forward pass.  A row's operands stay as they were loaded and are taken apart twice, for the sums and for dx: half the
@@ -262,7 +267,7 @@ template <typename T, bool KEEP> __device__ __forceinline__ void column_sums(con
 // 16384 x 1600 bf16 from 8-bit rows with the residual's gradient: 41.5 us and 4 of the join, 4.1 TB/s; from x without it 39 us, 4.0 TB/s; 32768 x 768 fp32
 // 54 us, 5.6 TB/s; 1000 x 1601 fp16 7.7 us.  What holds it below the forward pass is registers: the weight's gradient takes 16 for each octet, so a compute
 // unit has half the loads on their way.  Two rows ahead instead of one cost more in moves or wavefronts than they hid (57 to 67 us where this took 52).
-// Beyond 16384 columns the sums spill (1024 x 20000 bf16: 178 us).
+// 1024 x 20000 bf16: 87 us, 38 without the weight's gradient, whose columns are read a second time in pieces of 64 bytes.
 template <typename T, int L, int S, bool KEEP, bool COLUMNS> __global__ __launch_bounds__(threads_of(L)) void k_layernorm_backward(Backward f) {
     constexpr bool HELD = held(S);
     constexpr int R = HELD ? S : 1;  // octets that are held at a time
@@ -491,7 +496,13 @@ Launch columns_launch(int64_t rows, int lanes, int64_t cols) {
 // Either form, us, columns apart / along with the rows and a second launch: 32 x 768 3.6 / 8.2, 512 x 768 fp32 4.6 / 8.8, 1000 x 1600 bf16 6.4 / 10.7, 1000 x 64 5.4 /
 // 7.8, 1000 x 4096 11.6 / 14.7, 512 x 8192 16.1 / 18.4; but 2048 x 1024 8.8 / 9.4, 2048 x 300 12.0 / 7.9, 4096 x 1024 22 / 11, 1024 x 16384 71 / 42: a strip's workgroup
 // goes through all rows, and many strips wait for one another.
-bool by_columns(int64_t rows, int64_t cols) { return rows <= 4 * COMPUTE_UNITS && rows * cols <= static_cast<int64_t>(1) << 22; }
+// The sums of more than 16384 columns do not fit beside the row (with spilled registers 1024 x 20000 bf16 took 178 us where it takes 87).
+constexpr int64_t WIDEST = 16384, STRIP_ROWS = 1024;
+bool by_columns(int64_t rows, int64_t cols) { return cols > WIDEST || (rows <= 4 * COMPUTE_UNITS && rows * cols <= static_cast<int64_t>(1) << 22); }
+int strip_parts(int64_t rows) {
+    const int64_t parts = (rows + STRIP_ROWS - 1) / STRIP_ROWS;
+    return static_cast<int>(parts < COMPUTE_UNITS ? parts : COMPUTE_UNITS);
+}
 int64_t parts_at_most(int64_t rows, int64_t cols) {
     int64_t most = 0;
     with_shape<true>(cols, [&](auto, auto slots) { most = static_cast<int64_t>(COMPUTE_UNITS) * groups_per_unit(slots()); });
@@ -551,18 +562,20 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
     int parts = 0;
     float *partial = weights ? static_cast<float *>(workspace) : nullptr;
     if (rows > 0) {
-        Backward f{dy, x, weight, dsum, mean, rstd, dx, partial, dweight, dbias, accumulate, 0, 0, dy_stride, x_stride, dsum_stride, dx_stride, rows, cols,
+        Backward f{dy, x, weight, dsum, mean, rstd, dx, partial, dweight, dbias, accumulate, 0, 0, rows, dy_stride, x_stride, dsum_stride, dx_stride, rows, cols,
                    weight_dt != dt, act8_of(const_cast<void *>(act8), rows, cols)};
         with_type(dt, [&](auto *null) {
             using T = std::remove_pointer_t<decltype(null)>;
             with_shape<true>(cols, [&](auto lanes, auto slots) {
                 constexpr int L = decltype(lanes)::value, S = decltype(slots)::value;
-                const auto together = act8 != nullptr ? k_layernorm_backward<T, L, S, true, false> : k_layernorm_backward<T, L, S, false, false>;
+                constexpr bool APART = static_cast<int64_t>(L) * S * 8 > WIDEST;  // (no size would come to the other form)
+                const auto together = act8 != nullptr ? k_layernorm_backward<T, L, S, true, APART> : k_layernorm_backward<T, L, S, false, APART>;
                 const auto apart = act8 != nullptr ? k_layernorm_backward<T, L, S, true, true> : k_layernorm_backward<T, L, S, false, true>;
                 const bool columns = !weights || by_columns(rows, cols);
                 const Launch l = !columns ? launch_of(rows, L, groups_per_unit(S)) : weights ? columns_launch(rows, L, cols) : launch_of(rows, L, 2);
-                const int strips = columns && weights ? static_cast<int>((cols + STRIP - 1) / STRIP) : 0;
-                parts = columns ? 1 : l.groups;
+                const int shares = strip_parts(rows), strips = columns && weights ? static_cast<int>((cols + STRIP - 1) / STRIP) * shares : 0;
+                f.strip_rows = (rows + shares - 1) / shares;
+                parts = columns ? static_cast<int>((rows + f.strip_rows - 1) / f.strip_rows) : l.groups;
                 const auto launch = [&](int row_groups, int strip_groups) {
                     f.row_groups = row_groups;
                     f.strips = strip_groups;

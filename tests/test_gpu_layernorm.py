@@ -230,3 +230,34 @@ def test_more_elements_than_32_bits_count():
     d_h = ref.U * 4 * (np.abs(h) + 1)
     bound = ref.layernorm_backward_bounds(dy, h, d_h, r, np.ones(cols), np.zeros_like(dy), expected, torch.bfloat16)[0]
     assert (np.abs(ref.host(dx[picked]) - expected) <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_backward_of_many_rows_that_are_wide(dtype):
+    """Above 16384 columns the sums over the rows go in shares of at most 1024 rows: one and two of them, added to what is there, dx over dy."""
+    cols = 16401
+    for rows in (1024, 1030):
+        gen = torch.Generator(device="cuda").manual_seed(rows)
+        x, dy = ((torch.randn(rows, cols, device="cuda", generator=gen) + 0.25).to(dtype) for _ in range(2))
+        y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        buffer = B.new_act8(rows, cols)
+        B.adatopk_layernorm_forward(x, None, None, EPS, y, mean, rstd, act8=buffer)
+        kept = torch.empty(rows, cols, device="cuda")
+        B.adatopk_act8_load(buffer, kept)
+        ws = torch.empty(B.adatopk_layernorm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+        for keep in (False, True):
+            source = (None, buffer, None) if keep else (x, None, mean)
+            alone, dx = torch.empty_like(x), dy.clone()
+            B.adatopk_layernorm_backward(dy, *source, rstd, None, alone, None, None, None)
+            dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+            B.adatopk_layernorm_backward(dx, *source, rstd, None, dx, dw, db, ws)
+            assert torch.equal(dx, alone)
+            g = dy.double()
+            h = kept.double() if keep else (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+            # every term is rounded twice before it is added, the sum at most once for each row
+            error = (rows + 4) * 2.0 ** -24
+            assert bool(((dw - (g * h).sum(0)).abs() <= error * (g * h).abs().sum(0)).all())
+            assert bool(((db - g.sum(0)).abs() <= error * g.abs().sum(0)).all())
+            first_w, first_b = dw.clone(), db.clone()
+            B.adatopk_layernorm_backward(dy, *source, rstd, None, dx, dw, db, ws, accumulate=True)
+            assert torch.equal(dw, first_w + first_w) and torch.equal(db, first_b + first_b) and torch.equal(dx, alone)
