@@ -7,6 +7,7 @@ if the library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import warnings
 from typing import Optional, Sequence
@@ -521,7 +522,7 @@ def adatopk_plan_keep_counts(alpha: Sequence[float], beta: Sequence[float], n: S
 
 # ------------------------------------------------------------------ the training step of a stage around the link
 # A matrix is a tensor whose last dimension is contiguous and whose other dimensions are rows at one distance from the next: contiguous tensors of any
-# number of dimensions, and views that cut columns out of one.
+# number of dimensions, and views that cut columns out of one.  A tensor without elements is one whatever its strides.
 def _matrix(t: torch.Tensor, what: str):
     """(address, stride, rows, cols) of a tensor seen as rows of its last dimension."""
     if not t.is_cuda:
@@ -530,6 +531,8 @@ def _matrix(t: torch.Tensor, what: str):
     if not shape:
         raise ValueError("%s needs at least one dimension" % what)
     cols, strides = shape[-1], t.stride()
+    if 0 in shape:
+        return t.data_ptr(), cols, math.prod(shape[:-1]), cols
     if cols > 1 and strides[-1] != 1:
         raise ValueError("%s must be contiguous in its last dimension" % what)
     rows, stride = 1, cols

@@ -202,6 +202,7 @@ struct Call {
 };
 
 // A tensor seen as rows of its last dimension, which is contiguous: its other dimensions are rows at one distance from the next.
+// Without elements there is nothing to step over, whatever the strides.
 struct Matrix {
     void *data = nullptr;
     int64_t stride = 0, rows = 0, cols = 0;
@@ -218,12 +219,13 @@ struct Matrix {
         if (!c.plain) return;
         type = t.scalar_type();
         cols = t.size(dims - 1);
-        c.plain = cols <= 1 || t.stride(dims - 1) == 1;
+        const bool empty = t.numel() == 0;
+        c.plain = empty || cols <= 1 || t.stride(dims - 1) == 1;
         rows = 1;
         stride = cols;
         for (int64_t d = dims - 2; d >= 0 && c.plain; --d) {
             const int64_t size = t.size(d), step = t.stride(d);
-            if (size != 1) {
+            if (size != 1 && !empty) {
                 if (rows == 1)
                     stride = step;
                 else

@@ -1,0 +1,33 @@
+"""What the binding and the build of a stage's training step do before the device is touched; no GPU needed."""
+import pytest
+import torch
+
+from paper_2410_12707_amd import binding as B
+
+
+class Fake:
+    """What the binding looks at in a tensor on the device, from one in host memory."""
+
+    is_cuda = True
+
+    def __init__(self, t):
+        self.shape, self.dtype, self._t = t.shape, t.dtype, t
+
+    def stride(self):
+        return self._t.stride()
+
+    def data_ptr(self):
+        return self._t.data_ptr()
+
+
+@pytest.mark.parametrize("shape", [(0,), (0, 64), (3, 0), (3, 0, 64), (0, 3, 64), (2, 3, 0), (0, 0, 64), (2, 0, 5, 64), (2, 5, 0, 1)])
+def test_tensors_without_elements_are_matrices(shape):
+    # whatever dimension is empty and whatever the strides say: there is nothing to step over
+    rows = 1
+    for size in shape[:-1]:
+        rows *= size
+    for t in (torch.empty(shape), torch.empty(tuple(size + 2 for size in shape))[tuple(slice(0, size) for size in shape)], torch.empty(shape[::-1]).permute(*reversed(range(len(shape))))):
+        assert t.shape == torch.Size(shape) and B._matrix(Fake(t), "x")[2:] == (rows, shape[-1])
+        assert B._like(Fake(t), torch.float32, rows, shape[-1], "y") is not None
+    with pytest.raises(ValueError, match="y must be"):
+        B._like(Fake(torch.empty(shape)), torch.float32, rows + 1, shape[-1], "y")
