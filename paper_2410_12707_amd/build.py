@@ -5,6 +5,7 @@ kernels).  The product library carries none of them.  _marshal is the Python ext
 the arguments and makes the calls (marshal.cpp, host code only); the package works without it."""
 from __future__ import annotations
 
+import glob
 import os
 import subprocess
 import sysconfig
@@ -79,7 +80,9 @@ def marshal_is_stale() -> bool:
     if not os.path.exists(MARSHAL_LIB):
         return True
     t = os.path.getmtime(MARSHAL_LIB)
-    return any(os.path.getmtime(d) > t for d in (MARSHAL_SOURCE, HEADER))  # (it calls the library's functions by address, as the header declares them)
+    # it calls the library's functions by address, as the header declares them, and sizes buffers by the headers beside its source
+    beside = glob.glob(os.path.join(os.path.dirname(MARSHAL_SOURCE), "*.h"))
+    return any(os.path.getmtime(d) > t for d in [MARSHAL_SOURCE, HEADER] + beside)
 
 
 if __name__ == "__main__":

@@ -31,3 +31,25 @@ def test_tensors_without_elements_are_matrices(shape):
         assert B._like(Fake(t), torch.float32, rows, shape[-1], "y") is not None
     with pytest.raises(ValueError, match="y must be"):
         B._like(Fake(torch.empty(shape)), torch.float32, rows + 1, shape[-1], "y")
+
+
+def test_extension_is_rebuilt_after_a_change_of_the_layout(tmp_path, monkeypatch):
+    # the extension sizes 8-bit buffers by what the headers beside it say
+    import os
+
+    from paper_2410_12707_amd import build as b
+
+    used = [line.split('"')[1] for line in open(b.MARSHAL_SOURCE) if line.startswith('#include "')]
+    beside = [name for name in used if os.path.exists(os.path.join(os.path.dirname(b.MARSHAL_SOURCE), name))]
+    assert "act8_layout.h" in beside
+    for name in beside + ["wire_layout.h"]:  # (which the layout includes)
+        for path in tmp_path.iterdir():
+            path.unlink()
+        for path, attribute, time in (("marshal.cpp", "MARSHAL_SOURCE", 1), ("adatopk.h", "HEADER", 1), ("_marshal.so", "MARSHAL_LIB", 2), (name, None, 1)):
+            (tmp_path / path).write_text("")
+            os.utime(tmp_path / path, (time, time))
+            if attribute:
+                monkeypatch.setattr(b, attribute, str(tmp_path / path))
+        assert not b.marshal_is_stale(), name
+        os.utime(tmp_path / name, (3, 3))
+        assert b.marshal_is_stale(), name
