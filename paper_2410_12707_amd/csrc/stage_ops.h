@@ -251,7 +251,7 @@ __device__ __forceinline__ uint32_t group_exponent(const float (&v)[8]) {
     return e > 7 ? e : 7;
 }
 __device__ __forceinline__ U2 numbers(const float (&v)[8], uint32_t E) {
-    const float inverse = E == 255 ? 0.f : __uint_as_float((260u - E) << 23);
+    const float inverse = __uint_as_float((260u - E) << 23);
     uint32_t d[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -259,12 +259,12 @@ __device__ __forceinline__ U2 numbers(const float (&v)[8], uint32_t E) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float q = __builtin_rintf(v[4 * h + j] * inverse);
-            q = __builtin_amdgcn_fmed3f(q, -127.f, 127.f);  // (a NaN of a group that is marked anyway becomes a number)
+            q = __builtin_amdgcn_fmed3f(q, -127.f, 127.f);
             b[j] = static_cast<uint32_t>(static_cast<int32_t>(q));
         }
         d[h] = (b[0] & 0xFFu) | (b[1] & 0xFFu) << 8 | (b[2] & 0xFFu) << 16 | b[3] << 24;
     }
-    return U2{d[0], d[1]};
+    return E == 255 ? U2{0, 0} : U2{d[0], d[1]};  // (a marked group's numbers say nothing, and a padding behind a row that is no number stays one of zeros)
 }
 __device__ __forceinline__ float step_of(uint32_t E) { return E == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float((E > 7 ? E - 6 : 1) << 23); }
 __device__ __forceinline__ void values_of(U2 d, uint32_t E, float (&v)[8]) {

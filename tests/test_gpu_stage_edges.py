@@ -39,3 +39,40 @@ def test_tensors_without_elements(shape, either_way):
             assert bool((of_x == 0.0).all()) and bool((of_b == 0.0).all())
         torch.cuda.synchronize()
         assert bool((buffer == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_numbers_of_groups_without_a_scale_are_zeros(dtype):
+    # groups that hold a NaN or an infinity, and rows that layer norm makes NaN from end to end: E = 255, and the buffer is the same
+    # whatever the values were; behind a row's end there are zeros in any case
+    rows = 5
+    for cols in (1, 31, 33, 40, 64, 100, 700, 1601, 3000):
+        gen = torch.Generator(device="cuda").manual_seed(cols)
+        x = torch.randn(rows, cols, device="cuda", generator=gen).to(dtype)
+        x[1, cols // 2], x[3, cols - 1], x[3, 0] = float("nan"), float("inf"), -float("inf")
+        whole = torch.tensor([False, True, False, True, False], device="cuda")
+        groups, n = (cols + 31) // 32, B.adatopk_act8_bytes(rows, cols)
+        marked = torch.zeros(rows, groups, dtype=torch.bool, device="cuda")
+        marked[1, cols // 2 // 32] = marked[3, (cols - 1) // 32] = marked[3, 0] = True
+
+        def split(buffer):
+            q = buffer[:rows * groups * 32].view(torch.int8).view(rows, groups, 32)
+            return q, buffer[n - rows * groups:].view(rows, groups)
+
+        def check(buffer, where):
+            q, e = split(buffer)
+            assert torch.equal(e == 255, where), cols
+            assert bool((q[where] == 0).all()), cols
+            assert bool((q.reshape(rows, -1)[:, cols:] == 0).all()), cols
+
+        buffers = [torch.full((n,), 0xAB, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        B.adatopk_act8_store(x, buffers[0])
+        check(buffers[0], marked)
+        y = torch.empty_like(x)
+        B.adatopk_gelu_forward(x.abs(), y, *buffers)  # (GELU of an infinity is one)
+        check(buffers[0], marked)
+        check(buffers[1], marked)
+        B.adatopk_layernorm_forward(x, None, None, 1e-5, y, None, None, act8=buffers[0])
+        check(buffers[0], whole[:, None].expand(rows, groups))
+        B.adatopk_layernorm_forward(torch.full_like(x, 2.0), None, None, 0.0, y, None, None, act8=buffers[0])  # no variance and no eps: 0 / 0
+        check(buffers[0], torch.ones_like(marked))
