@@ -280,9 +280,10 @@ adatopk_status adatopk_plan_keep_counts(const double *alpha, const double *beta,
  * scale (the layout that the OCP microscaling specification calls MXINT8).  With E = the exponent field, biased by 127 as in fp32, of
  * the group's largest magnitude, but at least 7, an element x is held as
  *     q = clamp(round_half_even(x / 2^(E - 133)), -127, 127)     and read back as     q * 2^(E - 133),
- * so the error is at most 1 / 127.5 of the group's largest magnitude, and the result does not depend on the machine.  E = 255 marks a group with a NaN
- * or an infinity; its numbers are zeros, and all of it reads back as NaN.  -0 is read back as +0.  The buffer: rows of numbers, each padded with zeros to a multiple of
- * 32; from the next multiple of 256 bytes on one byte E per group, row by row.  16-byte aligned. */
+ * so the error is at most 1 / 127.5 of the group's largest magnitude or, where E is held at 7 and the step at 2^-126, 2^-127; the result does not
+ * depend on the machine.  E = 255 marks a group with a NaN or an infinity; its numbers are zeros, and all of it reads back as NaN.  -0 is read back as
+ * +0.  The buffer: rows of numbers, each padded with zeros to a multiple of 32; from the next multiple of 256 bytes on one byte E per group, row by row.
+ * 16-byte aligned. */
 
 /* Host-only.  Bytes of the buffer of a rows x cols activation; 0 for invalid sizes. */
 size_t adatopk_act8_bytes(int64_t rows, int64_t cols);

@@ -232,7 +232,8 @@ template <typename T> __device__ __forceinline__ void store_row(T *p, int64_t le
 
 // ---- the 8-bit form.  E: the exponent field of the group's largest magnitude, at least 7 so that the step 2^(E - 133) and its inverse are
 // normal numbers; 255 where the group holds a NaN or an infinity.  x / step is exact (or far below a half), so a number is one rounding of the
-// value, whatever the machine; clamping +-128 to +-127 keeps number * step finite in every type and the error within amax / 127.5.
+// value, whatever the machine; clamping +-128 to +-127 keeps number * step finite in every type and the error within amax / 127.5
+// (within 2^-127 where the step is held at 2^-126).
 __device__ __forceinline__ uint32_t max_of_quad(uint32_t v) {
     // (quad_perm [1,0,3,2] and [2,3,0,1]: all four lanes take part, so callers keep whole quads active)
     uint32_t o = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0xB1, 0xF, 0xF, false));

@@ -1,7 +1,10 @@
-"""Calls of a stage's training step at the edges of what their description allows: tensors without elements."""
+"""Calls of a stage's training step at the edges of what their description allows: tensors without elements, values without a scale, the smallest
+values, precision as described."""
+import numpy as np
 import pytest
 import torch
 
+import stage_reference as ref
 from paper_2410_12707_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -76,3 +79,16 @@ def test_numbers_of_groups_without_a_scale_are_zeros(dtype):
         check(buffers[0], whole[:, None].expand(rows, groups))
         B.adatopk_layernorm_forward(torch.full_like(x, 2.0), None, None, 0.0, y, None, None, act8=buffers[0])  # no variance and no eps: 0 / 0
         check(buffers[0], torch.ones_like(marked))
+
+
+def test_groups_below_the_smallest_step():
+    # E stops at 7, so a step is 2^-126 at least: a group below 2^-120 is held with errors of up to 2^-127, whatever its largest magnitude
+    rng = np.random.default_rng(11)
+    for top in range(-149, -112):
+        x = ref.rounded(np.ldexp(1 + rng.random((3, 64)), top) * rng.choice([-1.0, 1.0], size=(3, 64)), torch.float32)
+        x[0, 0] = 2.0 ** top
+        buffer, y = B.new_act8(3, 64), torch.empty(3, 64, device="cuda")
+        B.adatopk_act8_store(ref.on_device(x, torch.float32), buffer)
+        B.adatopk_act8_load(buffer, y)
+        amax = np.abs(x).reshape(3, 2, 32).max(axis=2).repeat(32, axis=1)
+        assert (np.abs(ref.host(y) - x) <= np.maximum(amax / 127.5, 2.0 ** -127)).all(), top
