@@ -329,7 +329,8 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
                                           int32_t accumulate, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Gradient of a projection y = x W^T + b whose input was kept in 8 bits: dw = dy^T x (n_out rows of n_in floats, nothing between them),
- * db = sum over rows of dy.  Products are exact, sums fp32 in a fixed order.
+ * db = sum over rows of dy.  Products are exact as long as fp32 holds them as normal numbers, sums fp32 in a fixed order.  dy of fp32 is taken apart
+ * into three numbers of 8 bits, the smallest 2^-133: it is whole from 2^-110 on, and below loses what lies under 2^-133.
  *   dy           rows x n_out, type dt
  *   act8_x       the input, rows x n_in
  *   weight, bias n_in values each, or NULL: the input was weight * h + bias with h what act8_x holds (a layer norm's normalised rows), and x is
@@ -337,7 +338,7 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
  *   db           n_out floats, or NULL to skip
  *   accumulate   != 0: added to dw and db
  *   workspace    device, 256-byte aligned, at least adatopk_weight_grad_workspace_bytes(rows, n_out, n_in, dt)
- * n_out, n_in <= 131072, rows < 2^31. */
+ * n_out, n_in <= 131072, rows < 2^31.  n_out == 0 or n_in == 0: nothing is done, db is not written either. */
 size_t adatopk_weight_grad_workspace_bytes(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt);
 adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void *act8_x, int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt,
                                    const void *weight, const void *bias, adatopk_dtype weight_dt, float *dw, float *db, int32_t accumulate,

@@ -3,7 +3,7 @@
 // A matrix product whose long axis is the slow one of both operands.  Tiles of dY and X go through LDS as bf16, [token][feature], and come out
 // transposed (ds_read_b64_tr_b16), which is what the matrix instruction wants.  A number of the 8-bit form times its step, a power of two, is
 // exact in bf16; dY is taken apart into as many bf16 pieces as its type needs (bf16 one, fp16 two, fp32 three: the leading 8 bits, the next 8, the
-// rest), so every product is exact and the sums are 32-bit.
+// rest), so every product is exact and the sums are 32-bit (fp32 from 2^-110 on: below, the third piece ends at bf16's smallest number, 2^-133).
 //
 // With weight and bias of the layer norm whose normalised rows X holds, the projection's input was weight[k] * X + bias[k], so
 // dW[n][k] = weight[k] * (dY^T X)[n][k] + db[n] * bias[k]: two operations per result instead of a rounding per element of X.

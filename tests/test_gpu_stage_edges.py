@@ -92,3 +92,27 @@ def test_groups_below_the_smallest_step():
         B.adatopk_act8_load(buffer, y)
         amax = np.abs(x).reshape(3, 2, 32).max(axis=2).repeat(32, axis=1)
         assert (np.abs(ref.host(y) - x) <= np.maximum(amax / 127.5, 2.0 ** -127)).all(), top
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_gradients_down_to_the_smallest(dtype):
+    # one token, an input of ones or of 64: the result is the gradient, to the bit for 16-bit types and from 2^-110 on for fp32; below that what
+    # lies under 2^-133, the smallest number of its bf16 pieces, is cut off
+    rng = np.random.default_rng(12)
+    if dtype == torch.float32:
+        dy = torch.from_numpy((np.ldexp(1 + rng.random(8192), rng.integers(-149, 0, size=8192)) * rng.choice([-1.0, 1.0], size=8192)).astype(np.float32))
+    else:
+        dy = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(dtype)
+        dy = dy[torch.isfinite(dy) & (dy.float().abs() < 2.0 ** 100)]
+    dy = dy.view(1, -1).cuda()
+    n = dy.shape[1]
+    for value in (1.0, 64.0):
+        buffer = torch.from_numpy(ref.act8_buffer(np.full((1, 2), value))).cuda()
+        dw, db = torch.empty(n, 2, device="cuda"), torch.empty(n, device="cuda")
+        ws = torch.empty(B.adatopk_weight_grad_workspace_bytes(1, n, 2, dtype), dtype=torch.uint8, device="cuda")
+        B.adatopk_weight_grad(dy, buffer, dw, db, ws)
+        want = dy[0].double()
+        error = torch.zeros_like(want) if dtype != torch.float32 else torch.where(want.abs() < 2.0 ** -110, 2.0 ** -133, 0.0)
+        assert bool(((db.double() - want).abs() <= error).all())
+        for column in range(2):
+            assert bool(((dw[:, column].double() - value * want).abs() <= value * error).all())
