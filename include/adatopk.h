@@ -298,7 +298,8 @@ adatopk_status adatopk_act8_load(const void *act8, int64_t rows, int64_t cols, a
 adatopk_status adatopk_gelu_forward(const void *x, int64_t x_stride, int64_t rows, int64_t cols, adatopk_dtype dt, int32_t use_tanh, void *y,
                                     int64_t y_stride, void *act8_x, void *act8_y, void *hip_stream);
 
-/* dx = dy * GELU'(x), x as it reads back from act8_x.  dx may be dy itself (same stride). */
+/* dx = dy * GELU'(x), x as it reads back from act8_x.  dx may be dy itself (same stride).  Before the rounding to dt the slope GELU', which reaches from
+ * -0.13 to 1.13, is within 2^-21 for fp32 and within 2^-20 for 16-bit types, whose rounding is far coarser, and within 2^-18 with use_tanh. */
 adatopk_status adatopk_gelu_backward(const void *dy, int64_t dy_stride, const void *act8_x, int64_t rows, int64_t cols, adatopk_dtype dt,
                                      int32_t use_tanh, void *dx, int64_t dx_stride, void *hip_stream);
 

@@ -116,3 +116,22 @@ def test_gradients_down_to_the_smallest(dtype):
         assert bool(((db.double() - want).abs() <= error).all())
         for column in range(2):
             assert bool(((dw[:, column].double() - value * want).abs() <= value * error).all())
+
+
+@pytest.mark.parametrize("tanh", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_the_slope_of_gelu_as_closely_as_it_is_described(dtype, tanh):
+    # what the header says: 2^-21 of dy for fp32 and 2^-20 for 16-bit types, 2^-18 with the hyperbolic tangent, and the result's rounding.  Inputs: the
+    # grids of the 8-bit form from 2^-8 to 8, among them what lies next to the slope's zero
+    for scale in range(-8, 4):
+        x = np.arange(-127, 128).repeat(5)[:1280 - 5] * 2.0 ** (scale - 6)
+        x = np.concatenate([x, np.full(5, 127 * 2.0 ** (scale - 6))]).reshape(40, 32)
+        x[:, 0] = 2.0 ** scale * 127 / 64  # (every group has this grid)
+        held = ref.act8_encode(x)[2]
+        assert np.array_equal(held, x)
+        dy = ref.rounded(np.random.default_rng(scale + 20).uniform(1, 2, size=x.shape), dtype)
+        dx = torch.empty(x.shape, dtype=dtype, device="cuda")
+        B.adatopk_gelu_backward(ref.on_device(dy, dtype), torch.from_numpy(ref.act8_buffer(x)).cuda(), dx, tanh=tanh)
+        want = dy * ref.gelu_slope(x, tanh)
+        bound = dy * (2.0 ** -18 if tanh else 2.0 ** -21 if dtype == torch.float32 else 2.0 ** -20)
+        assert (np.abs(ref.host(dx) - want) <= bound + ref.HALF_ULP[dtype] * (np.abs(want) + bound) + ref.SMALLEST[dtype]).all(), scale
