@@ -57,6 +57,17 @@ void adatopk_measure_judge(int32_t missing_workgroups, int32_t wait_rounds);
 #define ADATOPK_MEASURE_PART_COUNTS 2
 size_t adatopk_measure_workspace_offset(int32_t what, int64_t n_total, int32_t num_segments, adatopk_dtype dtype);
 
+/* For tests of every form of a kernel: how a call of these sizes is cut up.  Host only, EINVAL for sizes that the call refuses or has nothing to
+ * do for.
+ *   weight_grad  out[0], out[1]  sides of a tile of results     out[2]  1: each load is bounded for itself (small matrices, rows far apart)
+ *                out[3]          shares of the tokens; more than one are joined by a second kernel
+ *   layernorm    out[0]          lanes to a row                 out[1]  octets of a row to a lane
+ *                out[2]          rows under way at a time
+ *                out[3]          backward pass with the weight's gradient: 0 if that is added up along with the rows, otherwise the number of
+ *                                shares of the rows in which it is, apart from them */
+adatopk_status adatopk_measure_weight_grad_cut(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, int64_t dy_stride, int32_t *out);
+adatopk_status adatopk_measure_layernorm_cut(int64_t rows, int64_t cols, int32_t backward, int32_t *out);
+
 /* Plain streaming kernels on `hip_stream`; all pointers are device memory, 16-byte
  * aligned; bytes must be a multiple of 16.
  *   copy:      dst[i] = src[i]                        (reads bytes, writes bytes)

@@ -70,6 +70,10 @@ def load_measure_library() -> ctypes.CDLL:
     lib.adatopk_measure_judge.restype = None
     lib.adatopk_measure_workspace_offset.argtypes = [i32, ctypes.c_int64, i32, i32]
     lib.adatopk_measure_workspace_offset.restype = sz
+    lib.adatopk_measure_weight_grad_cut.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, i32, ctypes.c_int64, p]
+    lib.adatopk_measure_weight_grad_cut.restype = i32
+    lib.adatopk_measure_layernorm_cut.argtypes = [ctypes.c_int64, ctypes.c_int64, i32, p]
+    lib.adatopk_measure_layernorm_cut.restype = i32
     lib.adatopk_measure_copy.argtypes = [p, p, sz, p]
     lib.adatopk_measure_copy.restype = i32
     lib.adatopk_measure_read_only.argtypes = [p, sz, p, p]
@@ -717,6 +721,21 @@ MEASURE_CLAIMS, MEASURE_CHUNK_COUNTS, MEASURE_PART_COUNTS = 0, 1, 2
 
 def measure_workspace_offset(what: int, n_total: int, num_segments: int, dtype: torch.dtype) -> int:
     return int(load_measure_library().adatopk_measure_workspace_offset(int(what), int(n_total), int(num_segments), _dtype_code(dtype)))
+
+
+def measure_weight_grad_cut(rows: int, n_out: int, n_in: int, dtype: torch.dtype, dy_stride: int):
+    """(sides of a tile, whether each load is bounded for itself, shares of the tokens) of a weight gradient."""
+    out = (ctypes.c_int32 * 4)()
+    _check(load_measure_library().adatopk_measure_weight_grad_cut(int(rows), int(n_out), int(n_in), _dtype_code(dtype), int(dy_stride), out),
+           "adatopk_measure_weight_grad_cut")
+    return (out[0], out[1]), bool(out[2]), out[3]
+
+
+def measure_layernorm_cut(rows: int, cols: int, backward: bool):
+    """(lanes to a row, octets to a lane, rows under way at a time, shares of the rows whose columns are added up apart or 0) of a layer norm."""
+    out = (ctypes.c_int32 * 4)()
+    _check(load_measure_library().adatopk_measure_layernorm_cut(int(rows), int(cols), 1 if backward else 0, out), "adatopk_measure_layernorm_cut")
+    return tuple(out)
 
 
 def measure_copy(dst: torch.Tensor, src: torch.Tensor) -> None:

@@ -9,6 +9,9 @@
 // are in 32 bits, the mean's in 64, and in a fixed order.  Memory bounds both passes on many rows; on few, the launch and the latency of load, sums and store.
 #include <hip/hip_runtime.h>
 
+#ifdef ADATOPK_MEASURE_BUILD
+#include "adatopk_measure.h"
+#endif
 #include "stage_ops.h"
 
 // Products and sums are fused where the code says so and nowhere else: the forms of the backward pass give the same bits.
@@ -484,6 +487,7 @@ Launch launch_of(int64_t rows, int lanes, int groups_per_unit) {
     const int64_t groups = (rows + teams - 1) / teams, most = static_cast<int64_t>(COMPUTE_UNITS) * groups_per_unit;
     return Launch{threads, static_cast<int>(groups < most ? groups : most)};
 }
+int forward_groups_per_unit(int slots) { return slots == 1 ? 4 : 2; }
 // Workgroups of the backward pass to a compute unit: each writes a partial sum, and one octet to a lane leaves registers for two.
 int groups_per_unit(int slots) { return slots == 1 ? 2 : 1; }
 // Of the form with columns apart: whole workgroups, which the columns need, and one to a compute unit, the columns' among them.
@@ -531,7 +535,7 @@ adatopk_status adatopk_layernorm_forward(const void *x, int64_t x_stride, const 
         using T = std::remove_pointer_t<decltype(null)>;
         with_shape<false>(cols, [&](auto lanes, auto slots) {
             constexpr int L = decltype(lanes)::value, S = decltype(slots)::value;
-            const Launch l = launch_of(rows, L, S == 1 ? 4 : 2);
+            const Launch l = launch_of(rows, L, forward_groups_per_unit(S));
             hipLaunchKernelGGL((k_layernorm_forward<T, L, S>), dim3(static_cast<unsigned>(l.groups)), dim3(static_cast<unsigned>(l.threads)), 0,
                                static_cast<hipStream_t>(hip_stream), f);
         });
@@ -596,5 +600,26 @@ adatopk_status adatopk_layernorm_backward(const void *dy, int64_t dy_stride, con
                            dweight, dbias, accumulate);
     return launched();
 }
+
+#ifdef ADATOPK_MEASURE_BUILD
+adatopk_status adatopk_measure_layernorm_cut(int64_t rows, int64_t cols, int32_t backward, int32_t *out) {
+    if (!shape_ok(rows, cols) || cols > MAX_COLS || rows == 0 || cols == 0) return ADATOPK_EINVAL;
+    const bool columns = backward != 0 && by_columns(rows, cols);
+    const auto put = [&](auto lanes, auto slots) {
+        const Launch l = columns         ? columns_launch(rows, lanes(), cols)
+                         : backward != 0 ? launch_of(rows, lanes(), groups_per_unit(slots()))
+                                         : launch_of(rows, lanes(), forward_groups_per_unit(slots()));
+        out[0] = lanes();
+        out[1] = slots();
+        out[2] = l.groups * (l.threads / lanes());
+        out[3] = columns ? strip_parts(rows) : 0;
+    };
+    if (backward != 0)
+        with_shape<true>(cols, put);
+    else
+        with_shape<false>(cols, put);
+    return ADATOPK_OK;
+}
+#endif
 
 }  // extern "C"

@@ -11,6 +11,9 @@
 // Few tiles and many tokens: the tokens are split, partial products go to the workspace and k_weight_join adds them up in a fixed order.
 #include <hip/hip_runtime.h>
 
+#ifdef ADATOPK_MEASURE_BUILD
+#include "adatopk_measure.h"
+#endif
 #include "stage_ops.h"
 
 namespace {
@@ -471,6 +474,9 @@ Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, bool far
 
 constexpr int64_t MAX_FEATURES = 1 << 17;  // of either side: tiles, and rows of them, are counted in 32 bits
 
+// Whether rows of dY lie too far apart for them.
+bool far_apart(int64_t rows, int64_t dy_stride) { return rows > 1 && dy_stride >= MAX_STRIDE; }
+
 bool product_ok(int64_t rows, int64_t n_out, int64_t n_in) {
     return shape_ok(rows, n_in) && n_out >= 0 && n_out <= MAX_FEATURES && n_in <= MAX_FEATURES && rows < (static_cast<int64_t>(1) << 31);
 }
@@ -501,7 +507,7 @@ adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void
         !pointer_ok(workspace, 256) || (rows > 0 && (!matrix_ok(dy, dy_stride, rows, n_out, dt) || !pointer_ok(act8_x, 16))))
         return ADATOPK_EINVAL;
     if (workspace_bytes < adatopk_weight_grad_workspace_bytes(rows, n_out, n_in, dt)) return ADATOPK_EWORKSPACE;
-    const Cut c = cut_of(rows, n_out, n_in, dt, rows > 1 && dy_stride >= MAX_STRIDE);
+    const Cut c = cut_of(rows, n_out, n_in, dt, far_apart(rows, dy_stride));
     float *partial = static_cast<float *>(workspace);
     const bool wide = weight_dt == ADATOPK_F32;
     const Product f{dy,     dy_stride, act8_of(const_cast<void *>(act8_x), rows, n_in), rows, n_out, n_in, c.rows_per_split, c.tiles_in, c.tiles, c.split,
@@ -531,5 +537,17 @@ adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void
                            Join{f, Divisor(static_cast<uint32_t>(n_in)), weight_dt == ADATOPK_F16 ? 1 : 0});
     return launched();
 }
+
+#ifdef ADATOPK_MEASURE_BUILD
+adatopk_status adatopk_measure_weight_grad_cut(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, int64_t dy_stride, int32_t *out) {
+    if (!dtype_ok(dt) || !product_ok(rows, n_out, n_in) || n_out == 0 || n_in == 0) return ADATOPK_EINVAL;
+    const Cut c = cut_of(rows, n_out, n_in, dt, far_apart(rows, dy_stride));
+    out[0] = TILE_BM[c.tile];
+    out[1] = TILE_BN[c.tile];
+    out[2] = c.tile == TILE_SMALL ? 1 : 0;
+    out[3] = c.split;
+    return ADATOPK_OK;
+}
+#endif
 
 }  // extern "C"

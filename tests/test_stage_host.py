@@ -53,3 +53,47 @@ def test_extension_is_rebuilt_after_a_change_of_the_layout(tmp_path, monkeypatch
         assert not b.marshal_is_stale(), name
         os.utime(tmp_path / name, (3, 3))
         assert b.marshal_is_stale(), name
+
+
+def test_sizes_for_every_form_take_the_form_they_are_meant_for():
+    import stage_forms as forms
+
+    for dtype, tile, bounded, shared, (rows, n_out, n_in) in forms.WEIGHT_GRADIENTS:
+        cut = B.measure_weight_grad_cut(rows, n_out, n_in, dtype, n_out + 5)
+        assert cut[:2] == (tile, bounded) and (cut[2] > 1) == shared, (dtype, rows, n_out, n_in, cut)
+        assert rows % 64 != 0 and n_out % tile[0] != 0 and n_in % tile[1] != 0
+    for dtype, tile, (rows, n_out, n_in) in forms.MODEL_SIZES:
+        cut = B.measure_weight_grad_cut(rows, n_out, n_in, dtype, n_out)
+        assert cut[:2] == (tile, False), (dtype, rows, n_out, n_in, cut)
+    for table, backward in ((forms.BACKWARD, True), (forms.FORWARD, False)):
+        for lanes, octets, (rows, cols) in table:
+            cut = B.measure_layernorm_cut(rows, cols, backward)
+            assert cut[:2] == (lanes, octets) and cut[3] == 0 and cut[2] < rows and rows % cut[2] != 0, (rows, cols, cut)
+
+
+def test_there_is_no_other_form():
+    import random
+
+    import stage_forms as forms
+
+    rng = random.Random(3)
+
+    def size(most):
+        return max(1, int(round(most ** rng.random())))
+
+    tables = {dtype: {(tile, bounded, shared) for d, tile, bounded, shared, _ in forms.WEIGHT_GRADIENTS if d == dtype} for dtype in (forms.BF16, forms.F16, forms.F32)}
+    backward, forward = ({entry[:2] for entry in table} for table in (forms.BACKWARD, forms.FORWARD))
+    for _ in range(20000):
+        rows, n_out, n_in = size(70000), size(131072), size(131072)
+        for dtype, table in tables.items():
+            tile, bounded, split = B.measure_weight_grad_cut(rows, n_out, n_in, dtype, n_out)
+            assert (tile, bounded, split > 1) in table, (rows, n_out, n_in, dtype)
+        cols = size(32768)
+        lanes, octets, _, apart = B.measure_layernorm_cut(rows, cols, True)
+        assert apart or (lanes, octets) in backward, (rows, cols)
+        assert B.measure_layernorm_cut(rows, cols, False)[:2] in forward, (rows, cols)
+    # rows of dY too far apart for 32-bit offsets within a tile: each load bounded, whatever the size
+    for dtype in tables:
+        assert B.measure_weight_grad_cut(3000, 4096, 4096, dtype, (1 << 22) - 1)[1] is False
+        assert B.measure_weight_grad_cut(3000, 4096, 4096, dtype, 1 << 22)[1] is True
+        assert B.measure_weight_grad_cut(1, 4096, 4096, dtype, 1 << 40)[1] is False  # (with one row the stride is not looked at)
