@@ -70,6 +70,8 @@ __device__ __forceinline__ int place(int b, int n) {
 
 // A tile's results to where they belong: the weight's gradient, or with the tokens split the partial products.  A register holds four rows' results of 32
 // columns in each half of the wavefront, so a store's address is a scalar and an offset per lane.
+// Results that are added to what is there (accumulate) wait for a read each, behind the last product and with nothing beside it: 2048 tokens, 4096 x 1024,
+// bf16, 39.8 us without and 62.6 with; 16384 tokens, 6400 x 1600, 357 and 409.
 template <typename T, int BM, int BN, int WM, int WN, int MI, int NI, typename Block>
 __device__ __forceinline__ void finish(const Product &f, const F16v (&acc)[MI][NI], const float *sums, Block &&block, int64_t out0, int64_t own_out, int64_t in0,
                                        int64_t own_in, int part) {
