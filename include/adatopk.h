@@ -345,6 +345,70 @@ adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void
                                    const void *weight, const void *bias, adatopk_dtype weight_dt, float *dw, float *db, int32_t accumulate,
                                    void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ---- Projections in 8-bit floating point, the norm before them and the update of their weights.  Conventions as for the training step above.
+ *
+ * A matrix in 8-bit floating point (`fp8`): 128 consecutive elements of a row, the last block of a row being shorter, share a power of two as their scale.
+ * With m the block's largest magnitude, S is the smallest number, but at least 1, that has m <= 448 * 2^(S - 127); an element x is held as the number of
+ * the type E4M3 (four significand bits, exponents -6 ... 8, subnormals) nearest to x / 2^(S - 127), ties to even, and read back as that times 2^(S - 127).
+ * So the error is at most 2^-4 of the element or, below 2^-6 * 2^(S - 127), at most 2^-10 * 2^(S - 127).  S = 255 marks a block with a NaN or an infinity; all
+ * its numbers are NaN.  The buffer: rows of numbers, each padded with zeros to a multiple of 128; from the next multiple of 256 bytes on one byte S
+ * per block: those of the rows' first blocks, padded (with anything) to a multiple of 256 rows, then those of the second, and so on.  16-byte aligned.
+ * The scales are what the matrix instruction takes (E8M0), so a product costs nothing for them. */
+
+/* Host-only.  Bytes of the buffer of a rows x cols matrix; 0 for invalid sizes. */
+size_t adatopk_fp8_bytes(int64_t rows, int64_t cols);
+
+/* Puts a matrix away in 8-bit floating point, and reads it back as type dt. */
+adatopk_status adatopk_fp8_store(const void *x, int64_t x_stride, int64_t rows, int64_t cols, adatopk_dtype dt, void *fp8, void *hip_stream);
+adatopk_status adatopk_fp8_load(const void *fp8, int64_t rows, int64_t cols, adatopk_dtype dt, void *y, int64_t y_stride, void *hip_stream);
+
+/* Puts a weight matrix away with one scale for a tile of 128 x 128 (the blocks of 128 rows have equal S), as it is and transposed: either holds the same
+ * values, so the backward pass multiplies with the weights of the forward pass.
+ *   fp8             rows x cols, or NULL to skip
+ *   fp8_transposed  cols x rows, or NULL to skip; not both NULL */
+adatopk_status adatopk_fp8_store_weight(const void *w, int64_t w_stride, int64_t rows, int64_t cols, adatopk_dtype dt, void *fp8, void *fp8_transposed,
+                                        void *hip_stream);
+
+/* y = x W^T + bias + add: rows x n_out results of a projection, or with the transposed weights (n_in and n_out exchanged) the gradient of its input.  Products are
+ * exact, sums fp32 in a fixed order, rounded to dt once.
+ *   fp8_x        rows x n_in
+ *   fp8_w        n_out x n_in
+ *   bias         n_out values of bias_dt (dt or fp32), or NULL
+ *   add          rows x n_out values of dt, or NULL; may be y itself (same stride)
+ *   workspace    device, 256-byte aligned, at least adatopk_fp8_product_workspace_bytes(rows, n_out, n_in); not looked at where that is 0
+ * n_out, n_in <= 131072, rows < 2^31.  rows == 0 or n_out == 0: nothing is done.  n_in == 0: y = bias + add. */
+size_t adatopk_fp8_product_workspace_bytes(int64_t rows, int64_t n_out, int64_t n_in);
+adatopk_status adatopk_fp8_product(const void *fp8_x, const void *fp8_w, int64_t rows, int64_t n_out, int64_t n_in, const void *bias, adatopk_dtype bias_dt,
+                                   const void *add, int64_t add_stride, void *y, int64_t y_stride, adatopk_dtype dt, void *workspace, size_t workspace_bytes,
+                                   void *hip_stream);
+
+/* Root-mean-square norm of every row: s = x + residual, rounded to dt; rstd = 1 / sqrt(average of s^2 + eps); h = s * rstd; y = weight * h.  cols <= 32768.
+ *   residual     NULL: s = x
+ *   weight       NULL: ones
+ *   sum          s, or NULL to skip (only with a residual); may be x or residual itself (same stride)
+ *   y            NULL to skip where fp8 is given
+ *   rstd         `rows` floats, or NULL to skip
+ *   act8         h put away in 8-bit whole numbers, or NULL to skip: what the backward pass reads, and adatopk_weight_grad with the weight
+ *   fp8          y put away in 8-bit floating point (from before its rounding to dt), or NULL to skip: what adatopk_fp8_product reads
+ * y may be x or residual itself (same stride) where no sum is written there.  The average is taken in 64 bits, and h and y are put away as these formulas have
+ * them, without a rounding in between (where s is above 2^100, with rstd's to fp32). */
+adatopk_status adatopk_rmsnorm_forward(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight,
+                                       adatopk_dtype weight_dt, int64_t rows, int64_t cols, adatopk_dtype dt, float eps, void *sum, int64_t sum_stride, void *y,
+                                       int64_t y_stride, float *rstd, void *act8, void *fp8, void *hip_stream);
+
+/* Backward pass of the root-mean-square norm.  With g = dy * weight and the average over the row,
+ *     dx = rstd * (g - h * average(g * h)) + dsum,   dweight = sum over rows of dy * h.
+ *   x, act8      exactly one of the two: the normalised input s, from which h = s * rstd, or h in 8-bit whole numbers
+ *   dsum         gradient that reaches s on the residual path, or NULL
+ *   dx           may be dy or dsum itself (same stride)
+ *   dweight      `cols` floats, or NULL to skip; accumulate != 0 adds to them (the micro-batches before)
+ *   workspace    device, 256-byte aligned, at least adatopk_rmsnorm_backward_workspace_bytes(rows, cols); not looked at where dweight is NULL
+ * The order of all sums is fixed: equal calls give equal bits. */
+size_t adatopk_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
+adatopk_status adatopk_rmsnorm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *act8, const float *rstd, const void *weight,
+                                        adatopk_dtype weight_dt, const void *dsum, int64_t dsum_stride, int64_t rows, int64_t cols, adatopk_dtype dt, void *dx,
+                                        int64_t dx_stride, float *dweight, int32_t accumulate, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -166,6 +166,24 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.adatopk_weight_grad_workspace_bytes.restype = sz
     lib.adatopk_weight_grad.argtypes = [p, i64, p, i64, i64, i64, i32, p, p, i32, p, p, i32, p, sz, p]
     lib.adatopk_weight_grad.restype = i32
+    lib.adatopk_fp8_bytes.argtypes = [i64, i64]
+    lib.adatopk_fp8_bytes.restype = sz
+    lib.adatopk_fp8_store.argtypes = [p, i64, i64, i64, i32, p, p]
+    lib.adatopk_fp8_store.restype = i32
+    lib.adatopk_fp8_load.argtypes = [p, i64, i64, i32, p, i64, p]
+    lib.adatopk_fp8_load.restype = i32
+    lib.adatopk_fp8_store_weight.argtypes = [p, i64, i64, i64, i32, p, p, p]
+    lib.adatopk_fp8_store_weight.restype = i32
+    lib.adatopk_fp8_product_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.adatopk_fp8_product_workspace_bytes.restype = sz
+    lib.adatopk_fp8_product.argtypes = [p, p, i64, i64, i64, p, i32, p, i64, p, i64, i32, p, sz, p]
+    lib.adatopk_fp8_product.restype = i32
+    lib.adatopk_rmsnorm_forward.argtypes = [p, i64, p, i64, p, i32, i64, i64, i32, f32, p, i64, p, i64, p, p, p, p]
+    lib.adatopk_rmsnorm_forward.restype = i32
+    lib.adatopk_rmsnorm_backward_workspace_bytes.argtypes = [i64, i64]
+    lib.adatopk_rmsnorm_backward_workspace_bytes.restype = sz
+    lib.adatopk_rmsnorm_backward.argtypes = [p, i64, p, i64, p, p, p, i32, p, i64, i64, i64, i32, p, i64, p, i32, p, sz, p]
+    lib.adatopk_rmsnorm_backward.restype = i32
     lib.address = _Addresses(lib)
     return lib
 
@@ -696,6 +714,94 @@ def adatopk_weight_grad(dy: torch.Tensor, act8_x: torch.Tensor, dw: torch.Tensor
         address, stride, _act8(act8_x, rows, n_in, "act8_x"), rows, n_out, n_in, _dtype_code(dy.dtype), *_weights(weight, bias, dy.dtype, n_in), _dev(dw),
         _floats(db, n_out, "db"), 1 if accumulate else 0, _dev(workspace), workspace.numel() * workspace.element_size(), _stream()),
         "adatopk_weight_grad")
+
+
+# ------------------------------------------------------------------ projections in 8-bit floating point, the norm before them, the update of their weights
+def _fp8(t: torch.Tensor, rows: int, cols: int, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.uint8 or t.numel() < adatopk_fp8_bytes(rows, cols):
+        raise ValueError("%s must be uint8 with adatopk_fp8_bytes(%d, %d) entries" % (what, rows, cols))
+    return _dev(t)
+
+
+def adatopk_fp8_bytes(rows: int, cols: int) -> int:
+    return int(load_library().adatopk_fp8_bytes(int(rows), int(cols)))
+
+
+def new_fp8(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    """Buffer of a rows x cols matrix in 8-bit floating point."""
+    return torch.empty(max(adatopk_fp8_bytes(rows, cols), 16), dtype=torch.uint8, device=device)
+
+
+def adatopk_fp8_store(x: torch.Tensor, fp8: torch.Tensor) -> None:
+    """Puts a matrix away in 8-bit floating point, a scale for 128 elements of a row."""
+    lib = load_library()
+    address, stride, rows, cols = _matrix(x, "x")
+    _check(lib.adatopk_fp8_store(address, stride, rows, cols, _dtype_code(x.dtype), _fp8(fp8, rows, cols, "fp8"), _stream()), "adatopk_fp8_store")
+
+
+def adatopk_fp8_load(fp8: torch.Tensor, y: torch.Tensor) -> None:
+    """Reads a matrix of y's shape back."""
+    lib = load_library()
+    address, stride, rows, cols = _matrix(y, "y")
+    _check(lib.adatopk_fp8_load(_fp8(fp8, rows, cols, "fp8"), rows, cols, _dtype_code(y.dtype), address, stride, _stream()), "adatopk_fp8_load")
+
+
+def adatopk_fp8_store_weight(w: torch.Tensor, fp8: Optional[torch.Tensor], fp8_transposed: Optional[torch.Tensor] = None) -> None:
+    """Puts a weight matrix away with a scale for each tile of 128 x 128, as it is and transposed."""
+    lib = load_library()
+    address, stride, rows, cols = _matrix(w, "w")
+    _check(lib.adatopk_fp8_store_weight(address, stride, rows, cols, _dtype_code(w.dtype), _fp8(fp8, rows, cols, "fp8"),
+                                        _fp8(fp8_transposed, cols, rows, "fp8_transposed"), _stream()), "adatopk_fp8_store_weight")
+
+
+def adatopk_fp8_product_workspace_bytes(rows: int, n_out: int, n_in: int) -> int:
+    return int(load_library().adatopk_fp8_product_workspace_bytes(int(rows), int(n_out), int(n_in)))
+
+
+def adatopk_fp8_product(fp8_x: torch.Tensor, fp8_w: torch.Tensor, n_in: int, y: torch.Tensor, workspace: Optional[torch.Tensor],
+                        bias: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None) -> None:
+    """y = x W^T + bias + add, x and W from their 8 bits; n_in: the features of a row of either."""
+    lib = load_library()
+    n_in = int(n_in)
+    address, stride, rows, n_out = _matrix(y, "y")
+    _, bias_address, bias_code = _weights(None, bias, y.dtype, n_out)
+    _check(lib.adatopk_fp8_product(
+        _fp8(fp8_x, rows, n_in, "fp8_x"), _fp8(fp8_w, n_out, n_in, "fp8_w"), rows, n_out, n_in, bias_address, bias_code, *_like(add, y.dtype, rows, n_out, "add"),
+        address, stride, _dtype_code(y.dtype), None if workspace is None else _dev(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()), "adatopk_fp8_product")
+
+
+def adatopk_rmsnorm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, y: Optional[torch.Tensor], rstd: Optional[torch.Tensor],
+                            residual: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None, act8: Optional[torch.Tensor] = None,
+                            fp8: Optional[torch.Tensor] = None) -> None:
+    """y = root-mean-square norm of x + residual; the sum, the statistic, the divided rows and the weighted ones in 8 bits where buffers are given."""
+    lib = load_library()
+    address, stride, rows, cols = _matrix(x, "x")
+    weight_address, _, weight_code = _weights(weight, None, x.dtype, cols)
+    _check(lib.adatopk_rmsnorm_forward(
+        address, stride, *_like(residual, x.dtype, rows, cols, "residual"), weight_address, weight_code, rows, cols, _dtype_code(x.dtype), float(eps),
+        *_like(sum_out, x.dtype, rows, cols, "sum_out"), *_like(y, x.dtype, rows, cols, "y"), _floats(rstd, rows, "rstd"), _act8(act8, rows, cols, "act8"),
+        _fp8(fp8, rows, cols, "fp8"), _stream()), "adatopk_rmsnorm_forward")
+
+
+def adatopk_rmsnorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load_library().adatopk_rmsnorm_backward_workspace_bytes(int(rows), int(cols)))
+
+
+def adatopk_rmsnorm_backward(dy: torch.Tensor, x: Optional[torch.Tensor], act8: Optional[torch.Tensor], rstd: torch.Tensor, weight: Optional[torch.Tensor],
+                             dx: torch.Tensor, dweight: Optional[torch.Tensor], workspace: Optional[torch.Tensor], dsum: Optional[torch.Tensor] = None,
+                             accumulate: bool = False) -> None:
+    """Gradients of a root-mean-square norm from its input x or from its divided rows in 8 bits; dsum is added to dx."""
+    lib = load_library()
+    address, stride, rows, cols = _matrix(dy, "dy")
+    weight_address, _, weight_code = _weights(weight, None, dy.dtype, cols)
+    _check(lib.adatopk_rmsnorm_backward(
+        address, stride, *_like(x, dy.dtype, rows, cols, "x"), _act8(act8, rows, cols, "act8"), _floats(rstd, rows, "rstd"), weight_address, weight_code,
+        *_like(dsum, dy.dtype, rows, cols, "dsum"), rows, cols, _dtype_code(dy.dtype), *_like(dx, dy.dtype, rows, cols, "dx"), _floats(dweight, cols, "dweight"),
+        1 if accumulate else 0, None if workspace is None else _dev(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _stream()), "adatopk_rmsnorm_backward")
 
 
 # ------------------------------------------------------------------ measurement hooks (measuring build only)

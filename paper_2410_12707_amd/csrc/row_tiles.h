@@ -1,0 +1,235 @@
+// A tile of a product of two matrices whose rows lie along the sum, C[i][j] = sum over k of A[i][k] B[j][k], in 8-bit floating point with a scale for each 128 of a
+// row or in fp16.  Internal to the library.
+//
+// A step takes 128 bytes of every row of the tile, which go straight from memory into one of two buffers in LDS (no registers in between) while the matrix
+// instructions work on the other.  A load writes 64 x 16 bytes one behind the other, eight rows; which sixteen bytes of its row a lane fetches is turned by
+// the row's number, so that the lanes that read one place of eight rows together meet all banks.  One barrier per step; the first operands of a step are read
+// behind it and ahead of the last products of the step before, so the matrix unit has work across it.
+//
+// The 8-bit matrix instruction multiplies exactly and sums in fp32, but of each eight products it adds up first it drops what lies 2^-13 below the largest: results
+// are 1.3e-5 off in the root mean square of theirs, however long the sum (measured, 128 to 4096 terms of a normal distribution).  That is a sixteenth of fp16's rounding and
+// a hundredth of bf16's; for fp32 results the numbers are turned into bf16, scales applied, both exactly, and the 16-bit instruction sums them in fp32 throughout.
+#ifndef ADATOPK_ROW_TILES_H
+#define ADATOPK_ROW_TILES_H
+
+#include "stage_ops.h"
+
+namespace adatopk_stage {
+#if defined(__HIPCC__)
+
+typedef float F16v __attribute__((ext_vector_type(16)));
+typedef int I8v __attribute__((ext_vector_type(8)));
+typedef int I4v __attribute__((ext_vector_type(4)));
+typedef _Float16 H8v __attribute__((ext_vector_type(8)));
+typedef __bf16 B8v __attribute__((ext_vector_type(8)));
+typedef __bf16 B2v __attribute__((ext_vector_type(2)));
+
+constexpr int SLICE = 128;  // bytes of a row in a step
+
+// From global memory straight into LDS: 16 (4) bytes per lane, of all lanes if `lanes` is -1 and of none if it is 0, from base + offset, to `to` + 16 (4) *
+// lane.  All lanes of the wavefront are active around it.  Not waited for.  (Written out because the compiler waits for all of them before any read from
+// LDS; there is no register in it that could be taken for written too early.)
+__device__ __forceinline__ void copy_16(uint64_t base, uint32_t offset, uint32_t to, int lanes) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to),
+                 "v"(offset), "s"(base), "s"(lanes)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_4(uint64_t base, uint32_t offset, uint32_t to, int lanes) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to),
+                 "v"(offset), "s"(base), "s"(lanes)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void *)p));
+}
+template <int MORE> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(MORE) : "memory"); }
+// All that this wavefront has asked for is there, and every wavefront has come here.
+__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Eight numbers as bf16, times a power of two.
+__device__ __forceinline__ B8v bf16_of(int lo, int hi, float scale) {
+    const B2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const B2v c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return __builtin_shufflevector(__builtin_shufflevector(a, b, 0, 1, 2, 3), __builtin_shufflevector(c, d, 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ float power_of(int S) { return __uint_as_float(static_cast<uint32_t>(S < 254 ? S : 254) << 23); }  // (numbers under S = 255 are NaN themselves)
+
+enum Kind { HALF, FP8_FAST, FP8_EXACT };  // fp16; 8 bits by their own instruction; 8 bits as bf16
+
+// WM x WN wavefronts, an equal part of the tile each, in blocks of 32 x 32: of those, a lane holds column lane % 32 of B's side and, of A's, the rows
+// 8 * (q / 4) + 4 * (lane / 32) + q % 4.
+template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
+    static constexpr bool FP8 = KIND != HALF, EXACT = KIND == FP8_EXACT;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr int WAVES = WM * WN, NT = WAVES * 64, MI = BM / WM / 32, NI = BN / WN / 32;
+    static constexpr int STEPS = KIND == FP8_FAST ? 2 : 4, HALVES = EXACT ? 2 : 1;  // of a slice; matrix instructions along one
+    static constexpr int SCALES = FP8 ? 256 : 0;  // bytes for either side's scales: what a copy writes
+    static constexpr int BUFFER = (BM + BN) * SLICE + 2 * SCALES, LDS = 2 * BUFFER;
+    static constexpr int PA = BM / 8 / WAVES, PB = BN / 8 / WAVES;  // copies of a wavefront per slice
+    static_assert(PA >= 1 && PB >= 1 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && MI >= 1 && NI >= 1, "whole pieces");
+
+    // `source`: at_a(t), at_b(t): address of slice t of the tile's first row; pitch_a, pitch_b: bytes from one row to the next; left_a, left_b: rows from the
+    // tile's first one on (those behind are read as the last one); for FP8 scales_a(t), scales_b(t): addresses of the tile's scales of slice t.
+    template <typename Source> static __device__ __forceinline__ void run(char *lds, const Source &source, int slices, F16v (&acc)[MI][NI]) {
+        const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN, wn = wave % WN;
+        uint32_t from_a[PA], from_b[PB];
+        const uint32_t chunk = (lane % 8) ^ (lane / 8);
+#pragma unroll
+        for (int q = 0; q < PA; ++q) {
+            const int r = (wave * PA + q) * 8 + lane / 8, last = static_cast<int>(source.left_a) - 1;
+            from_a[q] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(source.pitch_a) + chunk * 16;
+        }
+#pragma unroll
+        for (int q = 0; q < PB; ++q) {
+            const int r = (wave * PB + q) * 8 + lane / 8, last = static_cast<int>(source.left_b) - 1;
+            from_b[q] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(source.pitch_b) + chunk * 16;
+        }
+        const uint32_t lds0 = lds_address(lds);
+        const uint32_t from_scales = lane * 4 < (wave < WAVES / 2 ? BM : BN) ? lane * 4 : 0;  // (what lies behind the tile's is not looked at)
+        // Copy number n of slice t's: the wavefront's eights of rows of A, of B, and the scales of A (half of the wavefronts write them, equal) or B.
+        constexpr int COPIES = PA + PB + (FP8 ? 1 : 0);
+        auto copy = [&](int n, int t, uint32_t to, int lanes) {
+            if (n < PA) {
+                copy_16(source.at_a(t), from_a[n < PA ? n : 0], to + (wave * PA + n) * 1024, lanes);
+            } else if (n < PA + PB) {
+                copy_16(source.at_b(t), from_b[n >= PA && n < PA + PB ? n - PA : 0], to + BM * SLICE + (wave * PB + n - PA) * 1024, lanes);
+            } else if constexpr (FP8) {
+                const bool a = wave < WAVES / 2;
+                copy_4(a ? source.scales_a(t) : source.scales_b(t), from_scales, to + (BM + BN) * SLICE + (a ? 0 : SCALES), lanes);
+            }
+        };
+        // An operand's place: row lane % 32 of its block, sixteen bytes at a time, of which a slice has the ones below for each half of the wavefront.  Addresses
+        // move from buffer to buffer; what is not written so the compiler takes a register for.
+        constexpr int PLACES = 4;
+        uint32_t at[2][PLACES], scales = lds0 + (BM + BN) * SLICE + lane % 32;
+        typedef const __attribute__((address_space(3))) char Lds;
+#pragma unroll
+        for (int k = 0; k < PLACES; ++k) {
+            const uint32_t c = KIND == FP8_FAST ? 4 * (k / 2) + 2 * (lane / 32) + k % 2 : 2 * k + lane / 32;
+            at[0][k] = lds0 + (wm * (BM / WM) + lane % 32) * SLICE + (c ^ (lane % 8)) * 16;
+            at[1][k] = lds0 + BM * SLICE + (wn * (BN / WN) + lane % 32) * SLICE + (c ^ (lane % 8)) * 16;
+        }
+        auto pin = [&](uint32_t by) {
+#pragma unroll
+            for (int k = 0; k < PLACES; ++k) {
+                at[0][k] += by;
+                at[1][k] += by;
+                asm("" : "+v"(at[0][k]), "+v"(at[1][k]));
+            }
+            if constexpr (FP8) {
+                scales += by;
+                asm("" : "+v"(scales));
+            }
+        };
+        constexpr bool FAST = KIND == FP8_FAST;
+        I8v xa8[2][FAST ? MI : 1], xb8[2][FAST ? NI : 1];
+        H8v xa[2][KIND == HALF ? MI : 1], xb[2][KIND == HALF ? NI : 1];
+        I4v raw_a[EXACT ? MI : 1], raw_b[EXACT ? NI : 1];
+        B8v ya[2][2][EXACT ? MI : 1], yb[2][2][EXACT ? NI : 1];
+        int sa[FP8 ? MI : 1], sb[FP8 ? NI : 1], sa_next[FP8 ? MI : 1], sb_next[FP8 ? NI : 1];
+        // Operand n of a step, in the order in which the products want them: A's first block, B's, A's others.
+        constexpr int OPERANDS = MI + NI;
+        auto take = [&](int n, int step, int set) {
+            const bool a = n == 0 || n > NI;
+            const int k = n == 0 ? 0 : a ? n - NI : n - 1, side = a ? 0 : 1;
+            if (FP8 && step == 0)
+                (a ? sa_next[a ? k : 0] : sb_next[a ? 0 : k]) =
+                    *(const __attribute__((address_space(3))) uint8_t *)((Lds *)(uintptr_t)(scales + (a ? wm * (BM / WM) : SCALES + wn * (BN / WN))) + k * 32);
+            if constexpr (FAST) {
+                const I4v x = *(const __attribute__((address_space(3))) I4v *)((Lds *)(uintptr_t)at[side][2 * step] + k * 32 * SLICE);
+                const I4v y = *(const __attribute__((address_space(3))) I4v *)((Lds *)(uintptr_t)at[side][2 * step + 1] + k * 32 * SLICE);
+                (a ? xa8[set][a ? k : 0] : xb8[set][a ? 0 : k]) = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+            } else if constexpr (EXACT) {
+                (a ? raw_a[a ? k : 0] : raw_b[a ? 0 : k]) = *(const __attribute__((address_space(3))) I4v *)((Lds *)(uintptr_t)at[side][step] + k * 32 * SLICE);
+            } else {
+                (a ? xa[set][a ? k : 0] : xb[set][a ? 0 : k]) = *(const __attribute__((address_space(3))) H8v *)((Lds *)(uintptr_t)at[side][step] + k * 32 * SLICE);
+            }
+        };
+        // The operand, once it is there, in the form in which it is multiplied.
+        auto convert = [&](int n, int step, int set) {
+            const bool a = n == 0 || n > NI;
+            const int k = n == 0 ? 0 : a ? n - NI : n - 1;
+            if constexpr (EXACT) {
+                const I4v raw = a ? raw_a[a ? k : 0] : raw_b[a ? 0 : k];
+                if (step == 0) (a ? sa[a ? k : 0] : sb[a ? 0 : k]) = a ? sa_next[a ? k : 0] : sb_next[a ? 0 : k];
+                const float scale = power_of(a ? sa[a ? k : 0] : sb[a ? 0 : k]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) (a ? ya[set][h][a ? k : 0] : yb[set][h][a ? 0 : k]) = bf16_of(raw[2 * h], raw[2 * h + 1], scale);
+            }
+        };
+        auto multiply = [&](int m, int set) {
+            const int h = m / (MI * NI), i = m / NI % MI, j = m % NI;
+            if constexpr (FAST)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xa8[set][i], xb8[set][j], acc[i][j], 0, 0, 0, sa[i], 0, sb[j]);
+            else if constexpr (EXACT)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ya[set][h][i], yb[set][h][j], acc[i][j], 0, 0, 0);
+            else
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xa[set][i], xb[set][j], acc[i][j], 0, 0, 0);
+        };
+        // A slice: between two matrix instructions go the reads of the next step's operands and the copies of the slice after next, a few at a time (behind the
+        // last slice: reads of what is not looked at, and no copies).
+        auto slice = [&](int t, uint32_t now) {
+            constexpr int PRODUCTS = HALVES * MI * NI;
+            constexpr int BY = EXACT ? PRODUCTS / 2 : PRODUCTS > 4 ? PRODUCTS - 3 : PRODUCTS;  // the reads are done some products before their use
+            const int lanes = __builtin_amdgcn_readfirstlane(t + 2 < slices ? -1 : 0);
+            if constexpr (FAST) {
+#pragma unroll
+                for (int i = 0; i < MI; ++i) sa[i] = sa_next[i];
+#pragma unroll
+                for (int j = 0; j < NI; ++j) sb[j] = sb_next[j];
+            }
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const bool last = s + 1 == STEPS;
+#pragma unroll
+                for (int m = 0; m < PRODUCTS; ++m) {
+                    multiply(m, s % 2);
+                    if (last && m == 0) {
+                        wait_and_meet();
+                        pin(now == 0 ? BUFFER : 0u - BUFFER);
+                    }
+                    if (m < BY)
+#pragma unroll
+                        for (int n = m * OPERANDS / BY; n < (m + 1) * OPERANDS / BY; ++n) take(n, last ? 0 : s + 1, (s + 1) % 2);
+                    else if (EXACT)
+#pragma unroll
+                        for (int n = (m - BY) * OPERANDS / BY; n < (m - BY + 1) * OPERANDS / BY; ++n) convert(n, last ? 0 : s + 1, (s + 1) % 2);
+                    if (last)
+#pragma unroll
+                        for (int n = m * COPIES / PRODUCTS; n < (m + 1) * COPIES / PRODUCTS; ++n) copy(n, t + 2, lds0 + now, lanes);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        };
+        const int second = __builtin_amdgcn_readfirstlane(slices > 1 ? -1 : 0);
+#pragma unroll
+        for (int n = 0; n < COPIES; ++n) copy(n, 0, lds0, -1);
+#pragma unroll
+        for (int n = 0; n < COPIES; ++n) copy(n, 1, lds0 + BUFFER, second);
+        if (slices > 1)
+            wait_copies<COPIES>();
+        else
+            wait_copies<0>();
+        asm volatile("s_barrier" ::: "memory");
+        pin(0);
+#pragma unroll
+        for (int n = 0; n < OPERANDS; ++n) take(n, 0, 0);
+#pragma unroll
+        for (int n = 0; n < OPERANDS; ++n) convert(n, 0, 0);
+        uint32_t now = 0;
+        for (int t = 0; t < slices; ++t) {
+            slice(t, now);
+            now = BUFFER - now;
+        }
+    }
+};
+
+// Workgroup b of n works on place(b) of n: eight runs of neighbours, one for each XCD (workgroups go round the XCDs), so that tiles which read the same
+// rows share an L2.
+__device__ __forceinline__ int place(int b, int n) {
+    const int xcd = b % 8, per = n / 8, more = n % 8;
+    return xcd * per + (xcd < more ? xcd : more) + b / 8;
+}
+#endif  // __HIPCC__
+}  // namespace adatopk_stage
+#endif
