@@ -409,6 +409,22 @@ adatopk_status adatopk_rmsnorm_backward(const void *dy, int64_t dy_stride, const
                                         adatopk_dtype weight_dt, const void *dsum, int64_t dsum_stride, int64_t rows, int64_t cols, adatopk_dtype dt, void *dx,
                                         int64_t dx_stride, float *dweight, int32_t accumulate, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* A weight matrix changed by its orthogonalised gradient, as the optimiser Muon does; the gradient is what adatopk_weight_grad has added up.
+ *     m = mu * m + g;   u = m, or g + mu * m (nesterov != 0);   without a momentum u = g
+ *     X = u / (|u| + eps), |u| the Frobenius norm;   in each step   A = X X^T,  X = 3.4445 X + (-4.7750 A + 2.0315 A A) X
+ *     w = decay * w + scale * X     (decay 0: w is not read, only written; scale 1, decay 0: the orthogonalised gradient itself)
+ *   grad         rows x cols values of grad_dt
+ *   momentum     rows x cols floats, nothing between rows, read and written; or NULL
+ *   steps        1 ... 64; five take singular values from 0.01 ... 1 of |u| to 0.7 ... 1.2
+ *   w            rows x cols values of dt
+ *   workspace    device, 256-byte aligned, at least adatopk_muon_update_workspace_bytes(rows, cols)
+ * Everything between the steps carries 22 bits, sums are fp32 and |u| a 64-bit sum; w is rounded once.  A NaN or an infinity in u makes all of X NaN.
+ * rows, cols <= 65536, rows * cols < 2^31. */
+size_t adatopk_muon_update_workspace_bytes(int64_t rows, int64_t cols);
+adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatopk_dtype grad_dt, float *momentum, float mu, int32_t nesterov, int64_t rows,
+                                   int64_t cols, int32_t steps, float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

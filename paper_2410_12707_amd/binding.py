@@ -184,6 +184,10 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.adatopk_rmsnorm_backward_workspace_bytes.restype = sz
     lib.adatopk_rmsnorm_backward.argtypes = [p, i64, p, i64, p, p, p, i32, p, i64, i64, i64, i32, p, i64, p, i32, p, sz, p]
     lib.adatopk_rmsnorm_backward.restype = i32
+    lib.adatopk_muon_update_workspace_bytes.argtypes = [i64, i64]
+    lib.adatopk_muon_update_workspace_bytes.restype = sz
+    lib.adatopk_muon_update.argtypes = [p, i64, i32, p, f32, i32, i64, i64, i32, f32, p, i64, i32, f32, f32, p, sz, p]
+    lib.adatopk_muon_update.restype = i32
     lib.address = _Addresses(lib)
     return lib
 
@@ -802,6 +806,24 @@ def adatopk_rmsnorm_backward(dy: torch.Tensor, x: Optional[torch.Tensor], act8: 
         *_like(dsum, dy.dtype, rows, cols, "dsum"), rows, cols, _dtype_code(dy.dtype), *_like(dx, dy.dtype, rows, cols, "dx"), _floats(dweight, cols, "dweight"),
         1 if accumulate else 0, None if workspace is None else _dev(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
         _stream()), "adatopk_rmsnorm_backward")
+
+
+def adatopk_muon_update_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load_library().adatopk_muon_update_workspace_bytes(int(rows), int(cols)))
+
+
+def adatopk_muon_update(grad: torch.Tensor, momentum: Optional[torch.Tensor], mu: float, nesterov: bool, w: torch.Tensor, scale: float, decay: float,
+                        workspace: torch.Tensor, steps: int = 5, eps: float = 1e-7) -> None:
+    """w = decay * w + scale * (the orthogonalised gradient, or momentum, which takes its step first)."""
+    lib = load_library()
+    address, stride, rows, cols = _matrix(w, "w")
+    grad_address, grad_stride, grad_rows, grad_cols = _matrix(grad, "grad")
+    if (grad_rows, grad_cols) != (rows, cols):
+        raise ValueError("grad must have %d rows of %d" % (rows, cols))
+    _check(lib.adatopk_muon_update(
+        grad_address, grad_stride, _dtype_code(grad.dtype), _floats(momentum, rows * cols, "momentum"), float(mu), 1 if nesterov else 0, rows, cols, int(steps),
+        float(eps), address, stride, _dtype_code(w.dtype), float(scale), float(decay), _dev(workspace), workspace.numel() * workspace.element_size(), _stream()),
+        "adatopk_muon_update")
 
 
 # ------------------------------------------------------------------ measurement hooks (measuring build only)

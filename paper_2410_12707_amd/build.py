@@ -20,7 +20,7 @@ MEASURE_LIB = os.path.join(HERE, "libadatopk_measure.so")
 MARSHAL_LIB = os.path.join(HERE, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
 HEADER = os.path.join(ROOT, "include", "adatopk.h")
-SOURCES = [os.path.join(CSRC, name) for name in ("adatopk.hip", "act8.hip", "layernorm.hip", "rmsnorm.hip", "weight_grad.hip", "fp8.hip", "fp8_product.hip",
+SOURCES = [os.path.join(CSRC, name) for name in ("adatopk.hip", "act8.hip", "layernorm.hip", "rmsnorm.hip", "weight_grad.hip", "fp8.hip", "fp8_product.hip", "muon.hip",
                                              "adatopk_host.cpp")]
 INTERNAL_HEADERS = [os.path.join(CSRC, name) for name in ("wire_layout.h", "act8_layout.h", "fp8_layout.h", "stage_ops.h", "norm.h", "fp8_form.h", "row_tiles.h")]
 

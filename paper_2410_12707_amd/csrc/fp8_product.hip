@@ -62,15 +62,6 @@ struct Source {
     __device__ __forceinline__ uint64_t scales_b(int t) const { return sb + static_cast<uint64_t>(t) * scale_pitch_b; }
 };
 
-// Tiles in bands of eight along the features, band by band, tokens within a band: the workgroups of an XCD that run at a time form a rectangle.
-constexpr int BAND = 8;
-__device__ __forceinline__ void tile_at(int tile, int tiles_out, int tiles_rows, int &out, int &row) {
-    const int band = tile / (BAND * tiles_rows), in = tile - band * BAND * tiles_rows;
-    const int width = tiles_out - band * BAND < BAND ? tiles_out - band * BAND : BAND;
-    row = in / width;
-    out = band * BAND + in - row * width;
-}
-
 template <typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Tile::NT, PER_CU * Tile::WAVES / 4) void k_fp8_product(Product f) {
     constexpr int MI = Tile::MI, NI = Tile::NI;
     constexpr int PITCH = MI * 32 + 4;  // floats from one token's results to the next in LDS
@@ -299,9 +290,9 @@ adatopk_status adatopk_fp8_product(const void *fp8_x, const void *fp8_w, int64_t
             return;
         }
         constexpr Kind KIND = sizeof(T) == 4 ? FP8_EXACT : FP8_FAST;
-        using Large = RowTile<KIND, 256, 256, 2, 2>;
-        using Middle = RowTile<KIND, 128, 128, 2, 2>;
-        using Small = RowTile<KIND, 64, 64, 2, 2>;
+        using Large = RowTile<KIND, 256, 256, 2, 2, 2>;
+        using Middle = RowTile<KIND, 128, 128, 2, 2, 2>;
+        using Small = RowTile<KIND, 64, 64, 2, 2, 2>;
         const dim3 groups(static_cast<unsigned>(c.tiles_out * c.tiles_rows * c.split));
         if (c.form == LARGE)
             hipLaunchKernelGGL((k_fp8_product<T, Large, 1>), groups, dim3(Large::NT), 0, st, f);

@@ -1,14 +1,17 @@
 // A tile of a product of two matrices whose rows lie along the sum, C[i][j] = sum over k of A[i][k] B[j][k], in 8-bit floating point with a scale for each 128 of a
-// row or in fp16.  Internal to the library.
+// row, or in pairs of fp16.  Internal to the library.
 //
-// A step takes 128 bytes of every row of the tile, which go straight from memory into one of two buffers in LDS (no registers in between) while the matrix
-// instructions work on the other.  A load writes 64 x 16 bytes one behind the other, eight rows; which sixteen bytes of its row a lane fetches is turned by
+// A step takes 128 bytes of every row of the tile, which go straight from memory into one of the buffers in LDS (no registers in between) while the matrix
+// instructions work on another.  A load writes 64 x 16 bytes one behind the other, eight rows; which sixteen bytes of its row a lane fetches is turned by
 // the row's number, so that the lanes that read one place of eight rows together meet all banks.  One barrier per step; the first operands of a step are read
 // behind it and ahead of the last products of the step before, so the matrix unit has work across it.
 //
 // The 8-bit matrix instruction multiplies exactly and sums in fp32, but of each eight products it adds up first it drops what lies 2^-13 below the largest: results
 // are 1.3e-5 off in the root mean square of theirs, however long the sum (measured, 128 to 4096 terms of a normal distribution).  That is a sixteenth of fp16's rounding and
 // a hundredth of bf16's; for fp32 results the numbers are turned into bf16, scales applied, both exactly, and the 16-bit instruction sums them in fp32 throughout.
+//
+// Pairs of fp16: x = h + l, l what the rounding to h left, rounded: 22 bits.  128 bytes of a row are 32 h and their 32 l, and a product is h h' + h l' + l h', what it
+// leaves off 2^-24 of it or less.
 #ifndef ADATOPK_ROW_TILES_H
 #define ADATOPK_ROW_TILES_H
 
@@ -26,25 +29,29 @@ typedef __bf16 B2v __attribute__((ext_vector_type(2)));
 
 constexpr int SLICE = 128;  // bytes of a row in a step
 
-// From global memory straight into LDS: 16 (4) bytes per lane, of all lanes if `lanes` is -1 and of none if it is 0, from base + offset, to `to` + 16 (4) *
-// lane.  All lanes of the wavefront are active around it.  Not waited for.  (Written out because the compiler waits for all of them before any read from
-// LDS; there is no register in it that could be taken for written too early.)
-__device__ __forceinline__ void copy_16(uint64_t base, uint32_t offset, uint32_t to, int lanes) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to),
-                 "v"(offset), "s"(base), "s"(lanes)
+// All lanes where a < b, none where not, for copies.  (By the scalar unit: a mask that comes out of vector instructions would have to wait before it is used.)
+__device__ __forceinline__ uint64_t lanes_if_less(int a, int b) {
+    uint64_t lanes;
+    asm volatile("s_cmp_lt_i32 %1, %2\n\ts_cselect_b64 %0, -1, 0" : "=s"(lanes) : "s"(a), "s"(b) : "scc");
+    return lanes;
+}
+// From global memory straight into LDS: 16 (4) bytes per lane of `lanes`, from base + offset, to `to` + 16 (4) * lane.  All lanes of the wavefront are active
+// around it.  Not waited for.  (Written out because the compiler waits for all of them before any read from LDS; there is no register in it that could be
+// taken for written too early.)
+__device__ __forceinline__ void copy_16(uint64_t base, uint32_t offset, uint32_t to, uint64_t lanes) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(offset), "s"(base), "s"(lanes)
                  : "memory");
 }
-__device__ __forceinline__ void copy_4(uint64_t base, uint32_t offset, uint32_t to, int lanes) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to),
-                 "v"(offset), "s"(base), "s"(lanes)
+__device__ __forceinline__ void copy_4(uint64_t base, uint32_t offset, uint32_t to, uint64_t lanes) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(offset), "s"(base), "s"(lanes)
                  : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void *)p));
 }
 template <int MORE> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(MORE) : "memory"); }
-// All that this wavefront has asked for is there, and every wavefront has come here.
-__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All that this wavefront has asked for but the last MORE copies is there, and every wavefront has come here.
+template <int MORE> __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(MORE) : "memory"); }
 
 // Eight numbers as bf16, times a power of two.
 __device__ __forceinline__ B8v bf16_of(int lo, int hi, float scale) {
@@ -54,17 +61,17 @@ __device__ __forceinline__ B8v bf16_of(int lo, int hi, float scale) {
 }
 __device__ __forceinline__ float power_of(int S) { return __uint_as_float(static_cast<uint32_t>(S < 254 ? S : 254) << 23); }  // (numbers under S = 255 are NaN themselves)
 
-enum Kind { HALF, FP8_FAST, FP8_EXACT };  // fp16; 8 bits by their own instruction; 8 bits as bf16
+enum Kind { PAIRS, FP8_FAST, FP8_EXACT };  // of fp16; 8 bits by their own instruction; 8 bits as bf16
 
 // WM x WN wavefronts, an equal part of the tile each, in blocks of 32 x 32: of those, a lane holds column lane % 32 of B's side and, of A's, the rows
 // 8 * (q / 4) + 4 * (lane / 32) + q % 4.
-template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
-    static constexpr bool FP8 = KIND != HALF, EXACT = KIND == FP8_EXACT;
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+template <Kind KIND, int BM_, int BN_, int WM_, int WN_, int STAGES_> struct RowTile {
+    static constexpr bool FP8 = KIND != PAIRS, EXACT = KIND == FP8_EXACT;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     static constexpr int WAVES = WM * WN, NT = WAVES * 64, MI = BM / WM / 32, NI = BN / WN / 32;
-    static constexpr int STEPS = KIND == FP8_FAST ? 2 : 4, HALVES = EXACT ? 2 : 1;  // of a slice; matrix instructions along one
+    static constexpr int STEPS = EXACT ? 4 : 2, TIMES = EXACT ? 2 : KIND == PAIRS ? 3 : 1;  // of a slice; matrix instructions of one
     static constexpr int SCALES = FP8 ? 256 : 0;  // bytes for either side's scales: what a copy writes
-    static constexpr int BUFFER = (BM + BN) * SLICE + 2 * SCALES, LDS = 2 * BUFFER;
+    static constexpr int BUFFER = (BM + BN) * SLICE + 2 * SCALES, LDS = STAGES * BUFFER;
     static constexpr int PA = BM / 8 / WAVES, PB = BN / 8 / WAVES;  // copies of a wavefront per slice
     static_assert(PA >= 1 && PB >= 1 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && MI >= 1 && NI >= 1, "whole pieces");
 
@@ -88,7 +95,7 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
         const uint32_t from_scales = lane * 4 < (wave < WAVES / 2 ? BM : BN) ? lane * 4 : 0;  // (what lies behind the tile's is not looked at)
         // Copy number n of slice t's: the wavefront's eights of rows of A, of B, and the scales of A (half of the wavefronts write them, equal) or B.
         constexpr int COPIES = PA + PB + (FP8 ? 1 : 0);
-        auto copy = [&](int n, int t, uint32_t to, int lanes) {
+        auto copy = [&](int n, int t, uint32_t to, uint64_t lanes) {
             if (n < PA) {
                 copy_16(source.at_a(t), from_a[n < PA ? n : 0], to + (wave * PA + n) * 1024, lanes);
             } else if (n < PA + PB) {
@@ -105,7 +112,8 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
         typedef const __attribute__((address_space(3))) char Lds;
 #pragma unroll
         for (int k = 0; k < PLACES; ++k) {
-            const uint32_t c = KIND == FP8_FAST ? 4 * (k / 2) + 2 * (lane / 32) + k % 2 : 2 * k + lane / 32;
+            // (8 bits: a step's 32 bytes one behind the other, in two places; pairs: place 2 * step + piece)
+            const uint32_t c = KIND == FP8_FAST ? 4 * (k / 2) + 2 * (lane / 32) + k % 2 : EXACT ? 2 * k + lane / 32 : 4 * (k % 2) + 2 * (k / 2) + lane / 32;
             at[0][k] = lds0 + (wm * (BM / WM) + lane % 32) * SLICE + (c ^ (lane % 8)) * 16;
             at[1][k] = lds0 + BM * SLICE + (wn * (BN / WN) + lane % 32) * SLICE + (c ^ (lane % 8)) * 16;
         }
@@ -123,7 +131,7 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
         };
         constexpr bool FAST = KIND == FP8_FAST;
         I8v xa8[2][FAST ? MI : 1], xb8[2][FAST ? NI : 1];
-        H8v xa[2][KIND == HALF ? MI : 1], xb[2][KIND == HALF ? NI : 1];
+        H8v xa[2][2][KIND == PAIRS ? MI : 1], xb[2][2][KIND == PAIRS ? NI : 1];
         I4v raw_a[EXACT ? MI : 1], raw_b[EXACT ? NI : 1];
         B8v ya[2][2][EXACT ? MI : 1], yb[2][2][EXACT ? NI : 1];
         int sa[FP8 ? MI : 1], sb[FP8 ? NI : 1], sa_next[FP8 ? MI : 1], sb_next[FP8 ? NI : 1];
@@ -142,7 +150,10 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
             } else if constexpr (EXACT) {
                 (a ? raw_a[a ? k : 0] : raw_b[a ? 0 : k]) = *(const __attribute__((address_space(3))) I4v *)((Lds *)(uintptr_t)at[side][step] + k * 32 * SLICE);
             } else {
-                (a ? xa[set][a ? k : 0] : xb[set][a ? 0 : k]) = *(const __attribute__((address_space(3))) H8v *)((Lds *)(uintptr_t)at[side][step] + k * 32 * SLICE);
+#pragma unroll
+                for (int piece = 0; piece < 2; ++piece)
+                    (a ? xa[set][piece][a ? k : 0] : xb[set][piece][a ? 0 : k]) =
+                        *(const __attribute__((address_space(3))) H8v *)((Lds *)(uintptr_t)at[side][2 * step + piece] + k * 32 * SLICE);
             }
         };
         // The operand, once it is there, in the form in which it is multiplied.
@@ -164,14 +175,14 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
             else if constexpr (EXACT)
                 acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ya[set][h][i], yb[set][h][j], acc[i][j], 0, 0, 0);
             else
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xa[set][i], xb[set][j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xa[set][h == 2 ? 1 : 0][i], xb[set][h == 1 ? 1 : 0][j], acc[i][j], 0, 0, 0);
         };
-        // A slice: between two matrix instructions go the reads of the next step's operands and the copies of the slice after next, a few at a time (behind the
+        // A slice: between two matrix instructions go the reads of the next step's operands and the copies of the slice that comes into the buffer left, a few at a time (behind the
         // last slice: reads of what is not looked at, and no copies).
         auto slice = [&](int t, uint32_t now) {
-            constexpr int PRODUCTS = HALVES * MI * NI;
+            constexpr int PRODUCTS = TIMES * MI * NI;
             constexpr int BY = EXACT ? PRODUCTS / 2 : PRODUCTS > 4 ? PRODUCTS - 3 : PRODUCTS;  // the reads are done some products before their use
-            const int lanes = __builtin_amdgcn_readfirstlane(t + 2 < slices ? -1 : 0);
+            const uint64_t lanes = lanes_if_less(t + STAGES, slices);
             if constexpr (FAST) {
 #pragma unroll
                 for (int i = 0; i < MI; ++i) sa[i] = sa_next[i];
@@ -185,8 +196,12 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
                 for (int m = 0; m < PRODUCTS; ++m) {
                     multiply(m, s % 2);
                     if (last && m == 0) {
-                        wait_and_meet();
-                        pin(now == 0 ? BUFFER : 0u - BUFFER);
+                        // (what has been asked for and need not be there: the slices after the next one, if there are as many as buffers for them)
+                        if (STAGES > 2 && t + STAGES <= slices)
+                            wait_and_meet<(STAGES - 2) * COPIES>();
+                        else
+                            wait_and_meet<0>();
+                        pin(now == (STAGES - 1) * BUFFER ? 0u - (STAGES - 1) * BUFFER : BUFFER);
                     }
                     if (m < BY)
 #pragma unroll
@@ -196,18 +211,20 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
                         for (int n = (m - BY) * OPERANDS / BY; n < (m - BY + 1) * OPERANDS / BY; ++n) convert(n, last ? 0 : s + 1, (s + 1) % 2);
                     if (last)
 #pragma unroll
-                        for (int n = m * COPIES / PRODUCTS; n < (m + 1) * COPIES / PRODUCTS; ++n) copy(n, t + 2, lds0 + now, lanes);
+                        for (int n = m * COPIES / PRODUCTS; n < (m + 1) * COPIES / PRODUCTS; ++n) copy(n, t + STAGES, lds0 + now, lanes);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
         };
-        const int second = __builtin_amdgcn_readfirstlane(slices > 1 ? -1 : 0);
+        asm volatile("s_nop 4" ::: "memory");  // (an address that came out of the vector unit may be read by a load so much later; in the loop addresses are scalar sums)
 #pragma unroll
-        for (int n = 0; n < COPIES; ++n) copy(n, 0, lds0, -1);
+        for (int b = 0; b < STAGES; ++b) {
+            const uint64_t lanes = lanes_if_less(b, slices);
 #pragma unroll
-        for (int n = 0; n < COPIES; ++n) copy(n, 1, lds0 + BUFFER, second);
-        if (slices > 1)
-            wait_copies<COPIES>();
+            for (int n = 0; n < COPIES; ++n) copy(n, b, lds0 + b * BUFFER, lanes);
+        }
+        if (slices >= STAGES)
+            wait_copies<(STAGES - 1) * COPIES>();
         else
             wait_copies<0>();
         asm volatile("s_barrier" ::: "memory");
@@ -219,7 +236,7 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
         uint32_t now = 0;
         for (int t = 0; t < slices; ++t) {
             slice(t, now);
-            now = BUFFER - now;
+            now = now == (STAGES - 1) * BUFFER ? 0 : now + BUFFER;
         }
     }
 };
@@ -229,6 +246,14 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_> struct RowTile {
 __device__ __forceinline__ int place(int b, int n) {
     const int xcd = b % 8, per = n / 8, more = n % 8;
     return xcd * per + (xcd < more ? xcd : more) + b / 8;
+}
+// Tiles in bands of eight along one side, band by band, the other side within a band: the workgroups of an XCD that run at a time form a rectangle.
+constexpr int BAND = 8;
+__device__ __forceinline__ void tile_at(int tile, int tiles_a, int tiles_b, int &a, int &b) {
+    const int band = tile / (BAND * tiles_b), in = tile - band * BAND * tiles_b;
+    const int width = tiles_a - band * BAND < BAND ? tiles_a - band * BAND : BAND;
+    b = in / width;
+    a = band * BAND + in - b * width;
 }
 #endif  // __HIPCC__
 }  // namespace adatopk_stage
