@@ -198,7 +198,8 @@ class _Addresses:
     def __init__(self, lib: ctypes.CDLL):
         for name in ("compress", "decompress", "decompress_sorted", "decompress_accumulate", "decompress_segmented", "compress_wire",
                      "compress_wire_segmented", "decompress_wire", "compress_segmented", "act8_store", "act8_load", "gelu_forward", "gelu_backward",
-                     "layernorm_forward", "layernorm_backward", "weight_grad"):
+                     "layernorm_forward", "layernorm_backward", "weight_grad", "fp8_store", "fp8_load", "fp8_store_weight", "fp8_product", "rmsnorm_forward",
+                     "rmsnorm_backward", "muon_update"):
             setattr(self, name, ctypes.cast(getattr(lib, "adatopk_" + name), ctypes.c_void_p).value)
 
 
@@ -262,7 +263,8 @@ def _check_pairs(dtype: torch.dtype, k_total: int, idx: torch.Tensor, val: torch
 _marshal = None  # the extension that reads the arguments and makes the calls; False: there is none
 _MARSHAL_NAMES = ("tensors", "int64s", "streams", "compress", "decompress", "compress_wire", "decompress_wire", "compress_segmented",
                   "decompress_segmented", "compress_wire_segmented", "act8_store", "act8_load", "gelu_forward", "gelu_backward", "layernorm_forward",
-                  "layernorm_backward", "weight_grad")
+                  "layernorm_backward", "weight_grad", "fp8_store", "fp8_load", "fp8_store_weight", "fp8_product", "rmsnorm_forward", "rmsnorm_backward",
+                  "muon_update")
 
 
 def _load_marshal():
@@ -741,6 +743,9 @@ def new_fp8(rows: int, cols: int, device="cuda") -> torch.Tensor:
 def adatopk_fp8_store(x: torch.Tensor, fp8: torch.Tensor) -> None:
     """Puts a matrix away in 8-bit floating point, a scale for 128 elements of a row."""
     lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.fp8_store(lib.address.fp8_store, x, fp8), "adatopk_fp8_store"):
+        return
     address, stride, rows, cols = _matrix(x, "x")
     _check(lib.adatopk_fp8_store(address, stride, rows, cols, _dtype_code(x.dtype), _fp8(fp8, rows, cols, "fp8"), _stream()), "adatopk_fp8_store")
 
@@ -748,6 +753,9 @@ def adatopk_fp8_store(x: torch.Tensor, fp8: torch.Tensor) -> None:
 def adatopk_fp8_load(fp8: torch.Tensor, y: torch.Tensor) -> None:
     """Reads a matrix of y's shape back."""
     lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.fp8_load(lib.address.fp8_load, fp8, y), "adatopk_fp8_load"):
+        return
     address, stride, rows, cols = _matrix(y, "y")
     _check(lib.adatopk_fp8_load(_fp8(fp8, rows, cols, "fp8"), rows, cols, _dtype_code(y.dtype), address, stride, _stream()), "adatopk_fp8_load")
 
@@ -755,6 +763,9 @@ def adatopk_fp8_load(fp8: torch.Tensor, y: torch.Tensor) -> None:
 def adatopk_fp8_store_weight(w: torch.Tensor, fp8: Optional[torch.Tensor], fp8_transposed: Optional[torch.Tensor] = None) -> None:
     """Puts a weight matrix away with a scale for each tile of 128 x 128, as it is and transposed."""
     lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.fp8_store_weight(lib.address.fp8_store_weight, w, fp8, fp8_transposed), "adatopk_fp8_store_weight"):
+        return
     address, stride, rows, cols = _matrix(w, "w")
     _check(lib.adatopk_fp8_store_weight(address, stride, rows, cols, _dtype_code(w.dtype), _fp8(fp8, rows, cols, "fp8"),
                                         _fp8(fp8_transposed, cols, rows, "fp8_transposed"), _stream()), "adatopk_fp8_store_weight")
@@ -768,6 +779,9 @@ def adatopk_fp8_product(fp8_x: torch.Tensor, fp8_w: torch.Tensor, n_in: int, y: 
                         bias: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None) -> None:
     """y = x W^T + bias + add, x and W from their 8 bits; n_in: the features of a row of either."""
     lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.fp8_product(lib.address.fp8_product, fp8_x, fp8_w, n_in, y, workspace, bias, add), "adatopk_fp8_product"):
+        return
     n_in = int(n_in)
     address, stride, rows, n_out = _matrix(y, "y")
     _, bias_address, bias_code = _weights(None, bias, y.dtype, n_out)
@@ -782,6 +796,9 @@ def adatopk_rmsnorm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], eps
                             fp8: Optional[torch.Tensor] = None) -> None:
     """y = root-mean-square norm of x + residual; the sum, the statistic, the divided rows and the weighted ones in 8 bits where buffers are given."""
     lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.rmsnorm_forward(lib.address.rmsnorm_forward, x, weight, eps, y, rstd, residual, sum_out, act8, fp8), "adatopk_rmsnorm_forward"):
+        return
     address, stride, rows, cols = _matrix(x, "x")
     weight_address, _, weight_code = _weights(weight, None, x.dtype, cols)
     _check(lib.adatopk_rmsnorm_forward(
@@ -799,6 +816,9 @@ def adatopk_rmsnorm_backward(dy: torch.Tensor, x: Optional[torch.Tensor], act8: 
                              accumulate: bool = False) -> None:
     """Gradients of a root-mean-square norm from its input x or from its divided rows in 8 bits; dsum is added to dx."""
     lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.rmsnorm_backward(lib.address.rmsnorm_backward, dy, x, act8, rstd, weight, dx, dweight, workspace, dsum, accumulate), "adatopk_rmsnorm_backward"):
+        return
     address, stride, rows, cols = _matrix(dy, "dy")
     weight_address, _, weight_code = _weights(weight, None, dy.dtype, cols)
     _check(lib.adatopk_rmsnorm_backward(
@@ -816,6 +836,9 @@ def adatopk_muon_update(grad: torch.Tensor, momentum: Optional[torch.Tensor], mu
                         workspace: torch.Tensor, steps: int = 5, eps: float = 1e-7) -> None:
     """w = decay * w + scale * (the orthogonalised gradient, or momentum, which takes its step first)."""
     lib = load_library()
+    m = _marshal or _load_marshal()
+    if m and _done(m.muon_update(lib.address.muon_update, grad, momentum, mu, nesterov, w, scale, decay, workspace, steps, eps), "adatopk_muon_update"):
+        return
     address, stride, rows, cols = _matrix(w, "w")
     grad_address, grad_stride, grad_rows, grad_cols = _matrix(grad, "grad")
     if (grad_rows, grad_cols) != (rows, cols):

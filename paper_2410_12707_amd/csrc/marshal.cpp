@@ -19,6 +19,7 @@
 
 #include "act8_layout.h"
 #include "adatopk.h"
+#include "fp8_layout.h"
 
 namespace {
 
@@ -254,6 +255,15 @@ void *act8(Call &c, PyObject *o, int64_t rows, int64_t cols) {
     return c.buffer(o, at::ScalarType::Byte,
                     c.plain ? static_cast<int64_t>(adatopk_internal::act8_exponents_at(rows, cols)) + rows * (adatopk_internal::act8_pitch(cols) / adatopk_internal::ACT8_GROUP)
                             : 0);
+}
+void *fp8(Call &c, PyObject *o, int64_t rows, int64_t cols) {
+    if (o == Py_None) return nullptr;
+    if (!adatopk_internal::fp8_shape_ok(rows, cols)) c.plain = false;
+    return c.buffer(o, at::ScalarType::Byte, c.plain ? static_cast<int64_t>(adatopk_internal::fp8_bytes(rows, cols)) : 0);
+}
+float real(Call &c, PyObject *o) {
+    c.plain = c.plain && PyFloat_CheckExact(o);
+    return c.plain ? static_cast<float>(PyFloat_AS_DOUBLE(o)) : 0.f;
 }
 struct Weights {
     const void *weight = nullptr, *bias = nullptr;
@@ -546,6 +556,102 @@ PyObject *weight_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     });
 }
 
+// (fn, x, fp8)
+PyObject *fp8_store(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 3, [&](Call &c) -> long {
+        const Matrix x(c, a[1]);
+        const adatopk_dtype dt = c.dtype(x.type);
+        void *q = fp8(c, a[2], x.rows, x.cols), *stream = c.stream();
+        return without_gil<decltype(&adatopk_fp8_store)>(c, a[0], static_cast<const void *>(x.data), x.stride, x.rows, x.cols, dt, q, stream);
+    });
+}
+
+// (fn, fp8, y)
+PyObject *fp8_load(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 3, [&](Call &c) -> long {
+        const Matrix y(c, a[2]);
+        const adatopk_dtype dt = c.dtype(y.type);
+        void *q = fp8(c, a[1], y.rows, y.cols), *stream = c.stream();
+        return without_gil<decltype(&adatopk_fp8_load)>(c, a[0], static_cast<const void *>(q), y.rows, y.cols, dt, y.data, y.stride, stream);
+    });
+}
+
+// (fn, w, fp8 or None, fp8_transposed or None)
+PyObject *fp8_store_weight(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 4, [&](Call &c) -> long {
+        const Matrix w(c, a[1]);
+        const adatopk_dtype dt = c.dtype(w.type);
+        void *q = fp8(c, a[2], w.rows, w.cols), *t = fp8(c, a[3], w.cols, w.rows), *stream = c.stream();
+        return without_gil<decltype(&adatopk_fp8_store_weight)>(c, a[0], static_cast<const void *>(w.data), w.stride, w.rows, w.cols, dt, q, t, stream);
+    });
+}
+
+// (fn, fp8_x, fp8_w, n_in, y, workspace or None, bias or None, add or None)
+PyObject *fp8_product(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 8, [&](Call &c) -> long {
+        const Matrix y(c, a[4]), add(c, a[7], y);
+        const adatopk_dtype dt = c.dtype(y.type);
+        const int64_t n_in = c.number(a[3]);
+        void *x = fp8(c, a[1], y.rows, n_in), *w = fp8(c, a[2], y.cols, n_in);
+        const Weights b(c, Py_None, a[6], y.type, y.cols);
+        const Workspace ws(c, a[5]);
+        void *stream = c.stream();
+        return without_gil<decltype(&adatopk_fp8_product)>(c, a[0], static_cast<const void *>(x), static_cast<const void *>(w), y.rows, y.cols, n_in, b.bias, b.type,
+                                                           static_cast<const void *>(add.data), add.stride, y.data, y.stride, dt, ws.data, ws.bytes, stream);
+    });
+}
+
+// (fn, x, weight or None, eps, y or None, rstd or None, residual or None, sum or None, act8 or None, fp8 or None)
+PyObject *rmsnorm_forward(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 10, [&](Call &c) -> long {
+        const Matrix x(c, a[1]), y(c, a[4], x), residual(c, a[6], x), sum(c, a[7], x);
+        const adatopk_dtype dt = c.dtype(x.type);
+        const Weights w(c, a[2], Py_None, x.type, x.cols);
+        const float eps = real(c, a[3]);
+        float *rstd = floats(c, a[5], x.rows);
+        void *q = act8(c, a[8], x.rows, x.cols), *e = fp8(c, a[9], x.rows, x.cols), *stream = c.stream();
+        return without_gil<decltype(&adatopk_rmsnorm_forward)>(c, a[0], static_cast<const void *>(x.data), x.stride, static_cast<const void *>(residual.data),
+                                                               residual.stride, w.weight, w.type, x.rows, x.cols, dt, eps, sum.data, sum.stride, y.data, y.stride,
+                                                               rstd, q, e, stream);
+    });
+}
+
+// (fn, dy, x or None, act8 or None, rstd, weight or None, dx, dweight or None, workspace or None, dsum or None, accumulate)
+PyObject *rmsnorm_backward(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 11, [&](Call &c) -> long {
+        const Matrix dy(c, a[1]), x(c, a[2], dy), dx(c, a[6], dy), dsum(c, a[9], dy);
+        const adatopk_dtype dt = c.dtype(dy.type);
+        const Weights w(c, a[5], Py_None, dy.type, dy.cols);
+        void *q = act8(c, a[3], dy.rows, dy.cols);
+        float *rstd = floats(c, a[4], dy.rows), *dw = floats(c, a[7], dy.cols);
+        const Workspace ws(c, a[8]);
+        const int accumulate = c.truth(a[10]);
+        void *stream = c.stream();
+        return without_gil<decltype(&adatopk_rmsnorm_backward)>(
+            c, a[0], static_cast<const void *>(dy.data), dy.stride, static_cast<const void *>(x.data), x.stride, static_cast<const void *>(q),
+            static_cast<const float *>(rstd), w.weight, w.type, static_cast<const void *>(dsum.data), dsum.stride, dy.rows, dy.cols, dt, dx.data, dx.stride, dw,
+            accumulate, ws.data, ws.bytes, stream);
+    });
+}
+
+// (fn, grad, momentum or None, mu, nesterov, w, scale, decay, workspace, steps, eps)
+PyObject *muon_update(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    return call(nargs, 11, [&](Call &c) -> long {
+        const Matrix grad(c, a[1]), w(c, a[5]);
+        c.plain = c.plain && grad.rows == w.rows && grad.cols == w.cols;
+        const adatopk_dtype grad_dt = c.dtype(grad.type), dt = c.dtype(w.type);
+        float *momentum = floats(c, a[2], c.plain ? w.rows * w.cols : 0);
+        const float mu = real(c, a[3]), scale = real(c, a[6]), decay = real(c, a[7]), eps = real(c, a[10]);
+        const int nesterov = c.truth(a[4]);
+        const Workspace ws(c, a[8]);
+        const int64_t steps = c.number(a[9]);
+        c.plain = c.plain && steps >= INT32_MIN && steps <= INT32_MAX;
+        void *stream = c.stream();
+        return without_gil<decltype(&adatopk_muon_update)>(c, a[0], static_cast<const void *>(grad.data), grad.stride, grad_dt, momentum, mu, nesterov, w.rows, w.cols,
+                                                           static_cast<int32_t>(steps), eps, w.data, w.stride, dt, scale, decay, ws.data, ws.bytes, stream);
+    });
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)> constexpr PyMethodDef fast(const char *name, const char *doc) {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(F)), METH_FASTCALL, doc};
 }
@@ -567,6 +673,13 @@ PyMethodDef methods[] = {
     fast<layernorm_forward>("layernorm_forward", "status of the call at an address, or None"),
     fast<layernorm_backward>("layernorm_backward", "status of the call at an address, or None"),
     fast<weight_grad>("weight_grad", "status of the call at an address, or None"),
+    fast<fp8_store>("fp8_store", "status of the call at an address, or None"),
+    fast<fp8_load>("fp8_load", "status of the call at an address, or None"),
+    fast<fp8_store_weight>("fp8_store_weight", "status of the call at an address, or None"),
+    fast<fp8_product>("fp8_product", "status of the call at an address, or None"),
+    fast<rmsnorm_forward>("rmsnorm_forward", "status of the call at an address, or None"),
+    fast<rmsnorm_backward>("rmsnorm_backward", "status of the call at an address, or None"),
+    fast<muon_update>("muon_update", "status of the call at an address, or None"),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "The calls of the library, their arguments read in C.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
