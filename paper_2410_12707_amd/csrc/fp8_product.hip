@@ -56,16 +56,15 @@ template <typename T> __device__ __forceinline__ void load_bias(const Product &f
 struct Source {
     uint64_t a, b, sa, sb;  // of the first slice
     int64_t pitch_a, pitch_b, left_a, left_b, scale_pitch_a, scale_pitch_b;
-    __device__ __forceinline__ uint64_t at_a(int t) const { return a + static_cast<uint64_t>(t) * SLICE; }
-    __device__ __forceinline__ uint64_t at_b(int t) const { return b + static_cast<uint64_t>(t) * SLICE; }
     __device__ __forceinline__ uint64_t scales_a(int t) const { return sa + static_cast<uint64_t>(t) * scale_pitch_a; }
     __device__ __forceinline__ uint64_t scales_b(int t) const { return sb + static_cast<uint64_t>(t) * scale_pitch_b; }
 };
 
-template <typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Tile::NT, PER_CU * Tile::WAVES / 4) void k_fp8_product(Product f) {
+template <typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Tile::NT, PER_CU * Tile::NT / 256) void k_fp8_product(Product f) {
     constexpr int MI = Tile::MI, NI = Tile::NI;
     constexpr int PITCH = MI * 32 + 4;  // floats from one token's results to the next in LDS
     constexpr int RESULTS = Tile::WAVES * 32 * PITCH * 4;
+    static_assert(Tile::ALONG == 1 || Tile::BN * PITCH * 4 <= Tile::GROUP_LDS, "a group's results fit its buffers");
     __shared__ __attribute__((aligned(16))) char lds[Tile::LDS > RESULTS ? Tile::LDS : RESULTS];
     const int tiles = f.tiles_out * f.tiles_rows, b = place(blockIdx.x, gridDim.x), part = b / tiles;
     int tile_out, tile_row;
@@ -82,43 +81,87 @@ template <typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Ti
     Tile::run(lds, source, slices, acc);
     __syncthreads();  // the buffers have been read
 
-    // Results through LDS, 32 tokens of a wavefront at a time: rows of y are written in whole lines.
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / Tile::WN, wn = wave % Tile::WN;
-    float *const mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
-    constexpr int OCTETS = MI * 4, AT_ONCE = 64 / OCTETS;
-    const int octet = lane % OCTETS, token = lane / OCTETS;
-    const int64_t col = out0 + wm * (Tile::BM / Tile::WM) + octet * 8;
-    float bias[8] = {};
-    if (f.split == 1 && col < f.n_out) load_bias<T>(f, col, bias);
-#pragma unroll
-    for (int j = 0; j < NI; ++j) {
+    // Results through LDS: rows of y are written in whole lines.  AT: octets that a thread has under way at a time.
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave % Tile::WAVES / Tile::WN, wn = wave % Tile::WN;
+    const auto lay = [&](float *to, int j) {  // a wavefront's results of 32 tokens
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 typedef float F4 __attribute__((ext_vector_type(4)));
-                *reinterpret_cast<F4 *>(mine + lane % 32 * PITCH + i * 32 + q * 8 + lane / 32 * 4) =
+                *reinterpret_cast<F4 *>(to + lane % 32 * PITCH + i * 32 + q * 8 + lane / 32 * 4) =
                     F4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
             }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        const int64_t row_at = row0 + wn * (Tile::BN / Tile::WN) + j * 32;
+    };
+    constexpr int OCTETS = MI * 4, AT = 4;
+    // Lines first, first + step, ... below `lines` of what `from` holds, GROUPS sums of each a distance apart; line 0 is token `row_at`.
+    const auto write = [&](auto groups, const float *from, int first, int step, int lines, int64_t row_at, int octet, int64_t col) {
+        constexpr int GROUPS = decltype(groups)::value, APART = Tile::GROUP_LDS / 4;
+        if (col >= f.n_out) return;
+        const int64_t left = f.n_out - col;
+        float bias[8] = {};
+        if (f.split == 1) load_bias<T>(f, col, bias);
+#pragma unroll 1
+        for (int k = first; k < lines; k += AT * step) {
+            float v[AT][8];
+            Raw<T> add[AT];
 #pragma unroll
-        for (int k = 0; k < 32; k += AT_ONCE) {
-            const int64_t row = row_at + k + token;
-            const U4 *const from = reinterpret_cast<const U4 *>(mine + (k + token) * PITCH + octet * 8);
-            const Raw<float> raw = {{from[0], from[1]}};
-            if (row >= f.rows || col >= f.n_out) continue;
-            if (f.split == 1) {
-                float v[8];
-                unpack(raw, v);
-                put<T>(f, row, col, bias, v);
-            } else {
-                store_row(f.partial + (part * f.rows + row) * f.n_out + col, f.n_out - col, raw);
+            for (int u = 0; u < AT; ++u) {
+                const int64_t row = row_at + k + u * step;
+                if (f.split == 1 && f.add != nullptr)
+                    add[u] = fetch_row(static_cast<const T *>(f.add) + row * f.add_stride + col, k + u * step < lines && row < f.rows ? left : 0, col > 0);
+                if (k + u * step >= lines) continue;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    const U4 *const at = reinterpret_cast<const U4 *>(from + g * APART + (k + u * step) * PITCH + octet * 8);
+                    float t[8];
+                    unpack(Raw<float>{{at[0], at[1]}}, t);
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) v[u][x] = g == 0 ? t[x] : v[u][x] + t[x];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < AT; ++u) {
+                const int64_t row = row_at + k + u * step;
+                if (k + u * step >= lines || row >= f.rows) continue;
+                if (f.split > 1) {
+                    store_row(f.partial + (part * f.rows + row) * f.n_out + col, left, pack<float>(v[u]));
+                    continue;
+                }
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[u][x] += bias[x];
+                if (f.add != nullptr) {
+                    float t[8];
+                    unpack(settle(add[u], left, col > 0), t);
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) v[u][x] += t[x];
+                }
+                store_row(static_cast<T *>(f.y) + row * f.y_stride + col, left, pack<T>(v[u]));
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+    };
+    if constexpr (Tile::ALONG > 1) {  // the groups' sums, added up in their order; the workgroup goes through the tile together
+        float *const sums = reinterpret_cast<float *>(lds);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) lay(sums + wave * (Tile::GROUP_LDS / 4) + j * 32 * PITCH, j);
+        __syncthreads();
+        const int octet = threadIdx.x % OCTETS;
+        write(std::integral_constant<int, Tile::ALONG>(), sums, threadIdx.x / OCTETS, Tile::NT / OCTETS, Tile::BN, row0, octet, out0 + octet * 8);
+    } else {
+        float *const mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
+        const auto together = [] {  // (a wavefront's lanes read what others of them have written)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        const int octet = lane % OCTETS;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            lay(mine, j);
+            together();
+            write(std::integral_constant<int, 1>(), mine, lane / OCTETS, 64 / OCTETS, 32, row0 + wn * (Tile::BN / Tile::WN) + j * 32, octet,
+                  out0 + wm * (Tile::BM / Tile::WM) + octet * 8);
+            together();
+        }
     }
 }
 
@@ -290,11 +333,14 @@ adatopk_status adatopk_fp8_product(const void *fp8_x, const void *fp8_w, int64_t
             return;
         }
         constexpr Kind KIND = sizeof(T) == 4 ? FP8_EXACT : FP8_FAST;
-        using Large = RowTile<KIND, 256, 256, 2, 2, 2>;
+        using Large = RowTile<KIND, 256, 256, 2, 4, 2>;
         using Middle = RowTile<KIND, 128, 128, 2, 2, 2>;
         using Small = RowTile<KIND, 64, 64, 2, 2, 2>;
+        using Deep = RowTile<KIND, 64, 64, 1, 1, 2, 4>;
         const dim3 groups(static_cast<unsigned>(c.tiles_out * c.tiles_rows * c.split));
-        if (c.form == LARGE)
+        if (c.form == SMALL && groups.x <= 256)
+            hipLaunchKernelGGL((k_fp8_product<T, Deep, 1>), groups, dim3(Deep::NT), 0, st, f);
+        else if (c.form == LARGE)
             hipLaunchKernelGGL((k_fp8_product<T, Large, 1>), groups, dim3(Large::NT), 0, st, f);
         else if (c.form == MIDDLE)
             hipLaunchKernelGGL((k_fp8_product<T, Middle, 2>), groups, dim3(Middle::NT), 0, st, f);

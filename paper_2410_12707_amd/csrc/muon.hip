@@ -7,9 +7,15 @@
 // symmetric, and X from B and X transposed, so each step writes X both ways; of A and B half the tiles are computed and written twice.
 //
 // Small singular values grow 3.4-fold in each step, and so does what a rounding of X leaves in their directions: with X in bf16 the result is some 2 to 7 % off, in
-// one fp16 1e-3 to 6e-3, in two fp16 4e-7 to 8e-6, like fp32 (512 to 1000 rows, of noise and of low rank with noise).  So everything between the steps is two fp16,
-// h + l, times 2^14 (A and X stay within 1.5, X's singular values within 1.21: nothing overflows, and l keeps its bits down to 2^-17) or, for B, whose diagonal
-// reaches 3.45, 2^13.  Products are three of the matrix instruction's, sums fp32; |u| is a 64-bit sum.
+// one fp16 1e-3 to 6e-3, in two fp16 4e-7 to 8e-6, like fp32 (512 to 1000 rows, of noise and of low rank with noise; 2-norm of the error, relative).  So
+// everything between the steps is two fp16, h + l, times 2^14 (A and X stay within 1.5, X's singular values within 1.21: nothing overflows, and l keeps its
+// bits down to 2^-17) or, for B, whose diagonal reaches 3.45, 2^13.  Products are three of the matrix instruction's, sums fp32; |u| is a 64-bit sum.
+//
+// With B X = a X + (b A + c A A) X only the first term matters where singular values are small: a step whose a X is added in the full 22 bits and whose products
+// are of the h alone leaves errors of some 2^-12 in directions that are large, and the steps behind it level most of them.  With all but the last three steps so,
+// the result is 6e-6 to 9e-5 off; with all but the last two, and the last one's products of the h alone, 4e-4 to 1e-3.  The first is taken where w is
+// fp16, whose own rounding is 2e-4 in the 2-norm, the second where it is bf16, whose rounding is 1.7e-3.  With fewer than 256 rows less is levelled (16 x 100:
+// 1.4e-3 and 4.3e-3 at the worst of eight) and products are not what takes the time: there all steps take the full 22 bits.
 #include <hip/hip_runtime.h>
 
 #include "row_tiles.h"
@@ -29,7 +35,7 @@ struct Pairs {
     uint8_t *at;
     int64_t pitch;
 };
-constexpr int64_t padded(int64_t n) { return (n + 31) / 32 * 32; }
+constexpr int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
 inline size_t pairs_bytes(int64_t rows, int64_t cols) { return adatopk_internal::align_up(static_cast<size_t>(rows) * static_cast<size_t>(padded(cols)) * 4, 256); }
 
 __device__ __forceinline__ uint8_t *octet_of(const Pairs &p, int64_t row, int64_t col) { return p.at + row * p.pitch + col / 32 * 128 + col % 32 * 2; }
@@ -145,15 +151,17 @@ template <typename G> __global__ __launch_bounds__(256) void k_muon_start(Start 
 }
 
 // ---- the steps' products
-enum Mode { GRAM, POLY, NEXT, LAST, SHARE };  // A = X X^T; B = a I + b A + c A A; X = B X; w = decay w + scale B X; partial sums of A = X X^T
+enum Mode { GRAM, POLY, NEXT, LAST, SHARE };  // A = X X^T; B = a I + b A + c A A; X = B X; w = decay w + scale B X; partial sums of X X^T or A A
 struct Product {
     Pairs a, b;             // operands: the result's [j][i], i of a's rows and j of b's
     int64_t rows_a, rows_b;
     int slices;             // of the whole sum
-    int tiles_a, tiles_b, slices_per_split;
+    int tiles_a, tiles_b, tiles, slices_per_split;
     Pairs by_j, by_i;       // the result as pairs, [j][i] and [i][j]
     Pairs gram;             // POLY: A
-    float *partial;         // SHARE: [split][rows][rows]
+    Pairs old_by_j, old_by_i;  // NEXT from the h alone: X as it was
+    float diagonal;         // POLY: a, or nothing where X a is added apart
+    float *partial;         // SHARE: [share][tile on and to one side of the diagonal][j][i], whole tiles
     void *w;
     int64_t w_stride;
     float scale, decay;
@@ -161,195 +169,329 @@ struct Product {
 struct Source {
     uint64_t a, b;
     int64_t pitch_a, pitch_b, left_a, left_b;
-    __device__ __forceinline__ uint64_t at_a(int t) const { return a + static_cast<uint64_t>(t) * SLICE; }
-    __device__ __forceinline__ uint64_t at_b(int t) const { return b + static_cast<uint64_t>(t) * SLICE; }
 };
 
-template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Tile::NT, PER_CU * Tile::WAVES / 4) void k_muon_product(Product f) {
+// Tiles on and to one side of the diagonal, row by row: row b has b + 1.
+__device__ __forceinline__ void tile_below(int tile, int &a, int &b) {
+    b = static_cast<int>((__builtin_sqrtf(8.f * static_cast<float>(tile) + 1.f) - 1.f) * 0.5f);
+    while (b * (b + 1) / 2 > tile) --b;
+    while ((b + 1) * (b + 2) / 2 <= tile) ++b;
+    a = tile - b * (b + 1) / 2;
+}
+// B's elements from A's and A A's, both as they are held: i and the seven behind it of row j.
+__device__ __forceinline__ void polynomial(const Product &f, int64_t j, int64_t i, float (&v)[8]) {
+    float gram[8] = {};
+    if (j < f.rows_b && i < padded(f.rows_a)) get_pairs(f.gram, j, i, gram);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        v[x] = __builtin_fmaf(v[x], NS_C * (ONE_OF_B / ONE / ONE), gram[x] * (NS_B * (ONE_OF_B / ONE)));
+        if (i + x == j) v[x] += f.diagonal * ONE_OF_B;
+    }
+}
+
+template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Tile::NT, PER_CU * Tile::NT / 256) void k_muon_product(Product f) {
     constexpr int MI = Tile::MI, NI = Tile::NI;
     constexpr int PITCH = MI * 32 + 4;  // floats from one j's results to the next in LDS
     constexpr int RESULTS = Tile::WAVES * 32 * PITCH * 4;
-    constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLY;
+    static_assert(Tile::ALONG == 1 || Tile::BN * PITCH * 4 <= Tile::GROUP_LDS, "a group's results fit its buffers");
+    constexpr bool SYMMETRIC = MODE == GRAM || MODE == POLY || MODE == SHARE;
     __shared__ __attribute__((aligned(16))) char lds[Tile::LDS > RESULTS ? Tile::LDS : RESULTS];
     int b = place(blockIdx.x, gridDim.x), part = 0, tile_a, tile_b;
-    if constexpr (SYMMETRIC) {  // tiles on and to one side of the diagonal: row b has b + 1
-        tile_b = static_cast<int>((__builtin_sqrtf(8.f * static_cast<float>(b) + 1.f) - 1.f) * 0.5f);
-        while (tile_b * (tile_b + 1) / 2 > b) --tile_b;
-        while ((tile_b + 1) * (tile_b + 2) / 2 <= b) ++tile_b;
-        tile_a = b - tile_b * (tile_b + 1) / 2;
+    if constexpr (SYMMETRIC) {
+        part = b / f.tiles;
+        b -= part * f.tiles;
+        tile_below(b, tile_a, tile_b);
     } else {
-        part = b / (f.tiles_a * f.tiles_b);
-        tile_at(b - part * f.tiles_a * f.tiles_b, f.tiles_a, f.tiles_b, tile_a, tile_b);
+        tile_at(b, f.tiles_a, f.tiles_b, tile_a, tile_b);
     }
     const int64_t a0 = static_cast<int64_t>(tile_a) * Tile::BM, b0 = static_cast<int64_t>(tile_b) * Tile::BN;
     const int first = part * f.slices_per_split, slices = f.slices - first < f.slices_per_split ? f.slices - first : f.slices_per_split;
-    const Source source{reinterpret_cast<uint64_t>(f.a.at + a0 * f.a.pitch + first * static_cast<int64_t>(SLICE)),
-                        reinterpret_cast<uint64_t>(f.b.at + b0 * f.b.pitch + first * static_cast<int64_t>(SLICE)), f.a.pitch, f.b.pitch,
+    const Source source{reinterpret_cast<uint64_t>(f.a.at + a0 * f.a.pitch + first * static_cast<int64_t>(Tile::STRIDE)),
+                        reinterpret_cast<uint64_t>(f.b.at + b0 * f.b.pitch + first * static_cast<int64_t>(Tile::STRIDE)), f.a.pitch, f.b.pitch,
                         f.rows_a - a0 < Tile::BM ? f.rows_a - a0 : Tile::BM, f.rows_b - b0 < Tile::BN ? f.rows_b - b0 : Tile::BN};
     F16v acc[MI][NI] = {};
     Tile::run(lds, source, slices, acc);
     __syncthreads();  // the buffers have been read
 
-    // Results through LDS, 32 j of a wavefront at a time: rows of either matrix are written sixteen bytes and more at a time.
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / Tile::WN, wn = wave % Tile::WN;
-    float *const mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
-    constexpr int OCTETS = MI * 4, AT_ONCE = 64 / OCTETS;
-    const int octet = lane % OCTETS, line = lane / OCTETS;
-    const int64_t i_at = a0 + wm * (Tile::BM / Tile::WM);
+    // Eight results of a j, i and the seven behind it: what becomes of them, and there they are for the other way of writing them.
+    const auto finish = [&](int64_t j, int64_t i, float (&v)[8]) {
+        if constexpr (MODE == GRAM || MODE == NEXT) {
 #pragma unroll
-    for (int n = 0; n < NI; ++n) {
-        const int64_t j_at = b0 + wn * (Tile::BN / Tile::WN) + n * 32;
+            for (int x = 0; x < 8; ++x) v[x] *= MODE == GRAM ? 1.f / ONE : 1.f / ONE_OF_B;
+            if constexpr (MODE == NEXT && Tile::FORM == HIGH) {
+                float old[8] = {};
+                if (j < f.rows_b && i < padded(f.rows_a)) get_pairs(f.old_by_j, j, i, old);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] = __builtin_fmaf(NS_A, old[x], v[x]);
+            }
+            if (j < f.rows_b) put_pairs(f.by_j, j, i, f.rows_a, v);
+        } else if constexpr (MODE == POLY) {
+            polynomial(f, j, i, v);
+            if (j < f.rows_b) put_pairs(f.by_j, j, i, f.rows_a, v);
+        } else if constexpr (MODE == SHARE) {
+            float *const to = f.partial + ((static_cast<int64_t>(part) * f.tiles + b) * Tile::BN + (j - b0)) * Tile::BM + (i - a0);
+            store_row(to, 8, pack<float>(v));
+        } else if (j < f.rows_b && i < f.rows_a) {
+            T *const to = static_cast<T *>(f.w) + j * f.w_stride + i;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x] *= f.scale * (1.f / ONE / ONE_OF_B);
+            if (f.decay != 0.f) {
+                float old[8];
+                unpack(load_row(to, f.rows_a - i, false), old);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] = __builtin_fmaf(f.decay, old[x], v[x]);
+            }
+            store_row(to, f.rows_a - i, pack<T>(v));
+        }
+    };
+    const bool both = MODE == NEXT || (MODE != SHARE && SYMMETRIC && tile_a != tile_b);  // whether [i][j] is written too
+
+    // Results through LDS: rows of either matrix are written sixteen bytes and more at a time.
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave % Tile::WAVES / Tile::WN, wn = wave % Tile::WN;
+    const auto lay = [&](float *to, int n) {  // a wavefront's results of 32 j
 #pragma unroll
         for (int m = 0; m < MI; ++m)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 typedef float F4 __attribute__((ext_vector_type(4)));
-                *reinterpret_cast<F4 *>(mine + lane % 32 * PITCH + m * 32 + q * 8 + lane / 32 * 4) =
+                *reinterpret_cast<F4 *>(to + lane % 32 * PITCH + m * 32 + q * 8 + lane / 32 * 4) =
                     F4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
             }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+    };
+    constexpr int OCTETS = MI * 4;
+    if constexpr (Tile::ALONG > 1) {  // the groups' sums, added up in their order; the workgroup goes through the tile together
+        constexpr int STEP = Tile::GROUP_LDS / 4;  // floats from one group's to the next
+        float *const sums = reinterpret_cast<float *>(lds);
 #pragma unroll
-        for (int k = 0; k < 32; k += AT_ONCE) {
-            const int64_t j = j_at + k + line, i = i_at + octet * 8;
-            U4 *const at = reinterpret_cast<U4 *>(mine + (k + line) * PITCH + octet * 8);
+        for (int n = 0; n < NI; ++n) lay(sums + wave * STEP + n * 32 * PITCH, n);
+        __syncthreads();
+#pragma unroll 2
+        for (int item = threadIdx.x; item < Tile::BN * OCTETS; item += Tile::NT) {
+            const int j = item / OCTETS, i = item % OCTETS * 8;
+            float v[8] = {};
+#pragma unroll
+            for (int g = 0; g < Tile::ALONG; ++g) {
+                const U4 *const at = reinterpret_cast<const U4 *>(sums + g * STEP + j * PITCH + i);
+                float t[8];
+                unpack(Raw<float>{{at[0], at[1]}}, t);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] += t[x];
+            }
+            finish(b0 + j, a0 + i, v);
+            if (both) {
+                const Raw<float> r = pack<float>(v);
+                U4 *const at = reinterpret_cast<U4 *>(sums + j * PITCH + i);
+                at[0] = r.w[0];
+                at[1] = r.w[1];
+            }
+        }
+        if constexpr (MODE == LAST || MODE == SHARE) return;
+        if (!both) return;
+        __syncthreads();
+#pragma unroll 2
+        for (int item = threadIdx.x; item < Tile::BM * (Tile::BN / 8); item += Tile::NT) {
+            const int i = item % Tile::BM, eight = item / Tile::BM * 8;
             float v[8];
-            unpack(Raw<float>{{at[0], at[1]}}, v);
-            if (j >= f.rows_b) continue;
-            if constexpr (MODE == GRAM) {
 #pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] *= 1.f / ONE;
-                put_pairs(f.by_j, j, i, f.rows_a, v);
-            } else if constexpr (MODE == POLY) {
-                float gram[8] = {};
-                if (i < padded(f.rows_a)) get_pairs(f.gram, j, i, gram);
+            for (int x = 0; x < 8; ++x) v[x] = sums[(eight + x) * PITCH + i];
+            if (a0 + i < f.rows_a) put_pairs(f.by_i, a0 + i, b0 + eight, f.rows_b, v);
+        }
+    } else {
+        const auto together = [] {  // (a wavefront's lanes read what others of them have written)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        float *const mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
+        const int64_t i_at = a0 + wm * (Tile::BM / Tile::WM);
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    v[x] = __builtin_fmaf(v[x], NS_C * (ONE_OF_B / ONE / ONE), gram[x] * (NS_B * (ONE_OF_B / ONE)));
-                    if (i + x == j) v[x] += NS_A * ONE_OF_B;
-                }
-                put_pairs(f.by_j, j, i, f.rows_a, v);
-                if (tile_a != tile_b) {
+        for (int n = 0; n < NI; ++n) {
+            const int64_t j_at = b0 + wn * (Tile::BN / Tile::WN) + n * 32;
+            lay(mine, n);
+            together();
+#pragma unroll 2
+            for (int item = lane; item < 32 * OCTETS; item += 64) {
+                const int k = item / OCTETS, octet = item % OCTETS;
+                U4 *const at = reinterpret_cast<U4 *>(mine + k * PITCH + octet * 8);
+                float v[8];
+                unpack(Raw<float>{{at[0], at[1]}}, v);
+                finish(j_at + k, i_at + octet * 8, v);
+                if (both) {
                     const Raw<float> r = pack<float>(v);
                     at[0] = r.w[0];
                     at[1] = r.w[1];
                 }
-            } else if constexpr (MODE == NEXT) {
+            }
+            together();
+            if constexpr (MODE != LAST && MODE != SHARE) {
+                if (both) {
+#pragma unroll 2
+                    for (int item = lane; item < MI * 128; item += 64) {  // an octet of j for an i
+                        const int i = item % (MI * 32), eight = item / (MI * 32) * 8;
+                        float v[8];
 #pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] *= 1.f / ONE_OF_B;
-                put_pairs(f.by_j, j, i, f.rows_a, v);
-            } else if constexpr (MODE == SHARE) {
-                if (i < f.rows_a) store_row(f.partial + (part * f.rows_b + j) * f.rows_a + i, f.rows_a - i, Raw<float>{{at[0], at[1]}});
-            } else {
-                if (i >= f.rows_a) continue;
-                T *const to = static_cast<T *>(f.w) + j * f.w_stride + i;
-#pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] *= f.scale * (1.f / ONE / ONE_OF_B);
-                if (f.decay != 0.f) {
-                    float old[8];
-                    unpack(load_row(to, f.rows_a - i, false), old);
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) v[x] = __builtin_fmaf(f.decay, old[x], v[x]);
+                        for (int x = 0; x < 8; ++x) v[x] = mine[(eight + x) * PITCH + i];
+                        if (i_at + i < f.rows_a) put_pairs(f.by_i, i_at + i, j_at + eight, f.rows_b, v);
+                    }
+                    together();
                 }
-                store_row(to, f.rows_a - i, pack<T>(v));
             }
         }
-        if constexpr (MODE == LAST || MODE == SHARE) {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            continue;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (!SYMMETRIC || tile_a != tile_b) {
-#pragma unroll
-            for (int k = 0; k < 2 * MI; ++k) {  // an octet of j for an i
-                const int item = k * 64 + lane, i = item % (MI * 32), eight = item / (MI * 32) * 8;
-                float v[8];
-#pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] = mine[(eight + x) * PITCH + i];
-                if (i_at + i >= f.rows_a) continue;
-                if constexpr (MODE != POLY)
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) v[x] *= MODE == GRAM ? 1.f / ONE : 1.f / ONE_OF_B;
-                put_pairs(f.by_i, i_at + i, j_at + eight, f.rows_b, v);
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
-// The shares of A added up in order.
-__global__ __launch_bounds__(256) void k_muon_join(const float *partial, int split, int64_t n, Pairs to, Divisor per_row, uint32_t octets) {
-    const uint32_t t = blockIdx.x * 256u + threadIdx.x;
-    if (t >= octets) return;
-    const uint32_t row = per_row.quotient(t);
-    const int64_t col = (t - row * per_row.d) * static_cast<int64_t>(8);
-    float v[8] = {};
-    for (int s = 0; s < split; ++s) {
-        float p[8];
-        unpack(load_row(partial + (s * n + row) * n + col, n - col, col > 0), p);
+// The shares of a symmetric product added up in order, 64 x 64 of a tile per workgroup, and what becomes of them (MODE: GRAM or POLY).
+template <Mode MODE> __global__ __launch_bounds__(256) void k_muon_join(Product f, int split, int side) {
+    __shared__ float tile[64][65];
+    const int per = side / 64, b = blockIdx.x / (per * per), sub = blockIdx.x % (per * per);
+    int tile_a, tile_b;
+    tile_below(b, tile_a, tile_b);
+    const int64_t i0 = sub % per * 64, j0 = sub / per * 64, a0 = static_cast<int64_t>(tile_a) * side + i0, b0 = static_cast<int64_t>(tile_b) * side + j0;
+    const bool both = tile_a != tile_b;
+    const int octet = threadIdx.x % 8;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += p[j];
+    for (int n = 0; n < 2; ++n) {
+        const int line = threadIdx.x / 8 + 32 * n;
+        const float *from = f.partial + (static_cast<int64_t>(b) * side + j0 + line) * side + i0 + octet * 8;
+        float v[8] = {};
+#pragma unroll 4
+        for (int s = 0; s < split; ++s) {
+            float t[8];
+            unpack(load_octet(from + static_cast<int64_t>(s) * f.tiles * side * side), t);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x] += t[x];
+        }
+        if constexpr (MODE == GRAM) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x] *= 1.f / ONE;
+        } else {
+            polynomial(f, b0 + line, a0 + octet * 8, v);
+        }
+        if (b0 + line < f.rows_b) put_pairs(f.by_j, b0 + line, a0 + octet * 8, f.rows_a, v);
+        if (both)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) tile[line][octet * 8 + x] = v[x];
     }
+    if (!both) return;
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= 1.f / ONE;
-    put_pairs(to, row, col, n, v);
+    for (int n = 0; n < 2; ++n) {
+        const int line = threadIdx.x / 8 + 32 * n;
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = tile[octet * 8 + x][line];
+        if (a0 + line < f.rows_a) put_pairs(f.by_i, a0 + line, b0 + octet * 8, f.rows_b, v);
+    }
 }
 
-using Large = RowTile<PAIRS, 256, 256, 2, 2, 2>;
-using Middle = RowTile<PAIRS, 128, 128, 2, 2, 2>;
-using Small = RowTile<PAIRS, 64, 64, 2, 2, 3>;
-
-// Which tile, and for the product of X with itself how many shares of the sum.
-struct Choice {
-    int side, split, per;
+// Tiles that there are kernels for.
+enum Shape { SHAPE_256, SHAPE_192, SHAPE_160, SHAPE_128, SHAPE_64, SHAPES };
+constexpr int SHAPE_BM[SHAPES] = {256, 192, 160, 128, 64}, SHAPE_BN[SHAPES] = {256, 256, 256, 128, 64}, SHAPE_SLOTS[SHAPES] = {256, 256, 256, 512, 768};
+template <Kind KIND> struct Tiles {
+    using Of256 = RowTile<KIND, 256, 256, 2, 4, 2>;
+    using Of192 = RowTile<KIND, 192, 256, 2, 4, 2>;
+    using Of160 = RowTile<KIND, 160, 256, 1, 4, 2>;
+    using Of128 = RowTile<KIND, 128, 128, 2, 2, 2>;
+    using Of64 = RowTile<KIND, 64, 64, 2, 2, 3>;
+    using Deep64 = RowTile<KIND, 64, 64, 1, 1, 2, 4>;  // where every tile has a compute unit to itself
 };
-constexpr int SPLIT_MAX = 32;
-Choice choice_of(int64_t rows_a, int64_t rows_b, int64_t sum, bool symmetric, bool shares) {
-    Choice best{0, 1, 0};
+
+// Which tile, whether the operands change places (then i is the second one's row), and for symmetric products how many shares of the sum.
+struct Choice {
+    Shape shape;
+    bool high, turned;
+    int split, per;
+};
+constexpr int SPLIT_MAX = 16;
+// us: of a slice on a full chip, from pairs (32 elements) and from the h alone (64, of which a compute unit fetches as many lines), and what a workgroup takes beside its
+// slices.  Measured on 1600 x 6400: X = B X from pairs 129, 115, 104, 115, 135 us by tile, from the h alone (and written as w) 64, 61, 65, 77, 109; X X^T
+// from pairs (with the join) 80, -, -, 68, 82, from the h alone 51, -, -, 48, 87; A A 45, -, -, 35, 30 and 34, -, -, 34, 24.
+constexpr double STEP[2][SHAPES] = {{2.3, 2.05, 1.85, 1.45, 0.72}, {2.0, 1.95, 2.1, 1.5, 1.1}}, BESIDE[SHAPES] = {14., 12., 11., 8., 5.};
+constexpr double DEEP_STEP = 0.17;  // of Deep64
+Choice choice_of(int64_t rows_a, int64_t rows_b, int64_t sum, bool symmetric, bool may_turn, bool high) {
+    Choice best{SHAPES, high, false, 1, 0};
     double least = 0;
-    const int slices = static_cast<int>(padded(sum) / 32);
-    for (const int side : {256, 128, 64}) {
-        const int64_t a = (rows_a + side - 1) / side, b = (rows_b + side - 1) / side;
-        const int units = side == 256 ? 256 : side == 128 ? 512 : 768;
-        const double step = side == 256 ? 1.6 : side == 128 ? 0.9 : 0.35, beside = side == 256 ? 10. : side == 128 ? 6. : 4.;
-        for (int split = 1; split <= (shares ? SPLIT_MAX : 1) && split <= slices; ++split) {
-            const int per = (slices + split - 1) / split;
-            if ((slices + per - 1) / per != split) continue;
-            const int64_t tiles = (symmetric && split == 1 ? a * (a + 1) / 2 : a * b) * split;
-            const double rounds = static_cast<double>((tiles + units - 1) / units);
-            const double cost = rounds * (beside + step * per) + (split == 1 ? 0. : 4. + 0.4e-6 * 4. * split * static_cast<double>(rows_a * rows_b));
-            if (best.side == 0 || cost < least) {
-                least = cost;
-                best = Choice{side, split, per};
+    const int slices = static_cast<int>(padded(sum) / (high ? 64 : 32));
+    for (int t = 0; t < SHAPES; ++t)
+        for (int turned = 0; turned < (may_turn && SHAPE_BM[t] != SHAPE_BN[t] ? 2 : 1); ++turned) {
+            if (symmetric && SHAPE_BM[t] != SHAPE_BN[t]) continue;
+            const int64_t a = ((turned ? rows_b : rows_a) + SHAPE_BM[t] - 1) / SHAPE_BM[t], b = ((turned ? rows_a : rows_b) + SHAPE_BN[t] - 1) / SHAPE_BN[t];
+            for (int split = 1; split <= (symmetric ? SPLIT_MAX : 1) && split <= slices; ++split) {
+                const int per = (slices + split - 1) / split;
+                if ((slices + per - 1) / per != split) continue;
+                const int64_t tiles = (symmetric ? a * (a + 1) / 2 : a * b) * split;
+                const bool deep = t == SHAPE_64 && tiles <= 256;
+                const double filled = static_cast<double>(tiles) / SHAPE_SLOTS[t];
+                // workgroups that share a compute unit slow one another down, and their rounds run into one another
+                const bool shared = SHAPE_SLOTS[t] > 256;
+                const double rounds = shared ? (filled < 1. ? 1. : 1.1 * filled) : static_cast<double>((tiles + SHAPE_SLOTS[t] - 1) / SHAPE_SLOTS[t]);
+                const double step = deep ? DEEP_STEP : STEP[high][t] * (shared && filled < 1. ? 0.5 + 0.5 * filled : 1.);
+                const double join = split == 1 ? 0. : 4. + 0.17e-6 * 4. * static_cast<double>(tiles) * SHAPE_BM[t] * SHAPE_BN[t];
+                const double cost = rounds * (BESIDE[t] + step * per) + join;
+                if (best.shape == SHAPES || cost < least) {
+                    least = cost;
+                    best = Choice{static_cast<Shape>(t), high, turned != 0, split, per};
+                }
             }
         }
-    }
     return best;
 }
 
-template <Mode MODE, typename T> void launch_product(Product f, int side, int split, hipStream_t st) {
-    f.tiles_a = static_cast<int>((f.rows_a + side - 1) / side);
-    f.tiles_b = static_cast<int>((f.rows_b + side - 1) / side);
-    const int64_t tiles = MODE == GRAM || MODE == POLY ? static_cast<int64_t>(f.tiles_a) * (f.tiles_a + 1) / 2 : static_cast<int64_t>(f.tiles_a) * f.tiles_b * split;
-    const dim3 groups(static_cast<unsigned>(tiles));
-    if (side == 256)
-        hipLaunchKernelGGL((k_muon_product<MODE, T, Large, 1>), groups, dim3(Large::NT), 0, st, f);
-    else if (side == 128)
-        hipLaunchKernelGGL((k_muon_product<MODE, T, Middle, 2>), groups, dim3(Middle::NT), 0, st, f);
-    else
-        hipLaunchKernelGGL((k_muon_product<MODE, T, Small, 3>), groups, dim3(Small::NT), 0, st, f);
+template <Mode MODE, typename T, Kind KIND> void launch_product(Product f, const Choice &c, hipStream_t st) {
+    using Of = Tiles<KIND>;
+    if (c.turned) {
+        const Pairs a = f.a, by_j = f.by_j;
+        const int64_t rows_a = f.rows_a;
+        f.a = f.b;
+        f.b = a;
+        f.rows_a = f.rows_b;
+        f.rows_b = rows_a;
+        f.by_j = f.by_i;
+        f.by_i = by_j;
+        f.old_by_j = f.old_by_i;
+    }
+    constexpr bool SYMMETRIC = MODE != NEXT && MODE != LAST;
+    f.tiles_a = static_cast<int>((f.rows_a + SHAPE_BM[c.shape] - 1) / SHAPE_BM[c.shape]);
+    f.tiles_b = static_cast<int>((f.rows_b + SHAPE_BN[c.shape] - 1) / SHAPE_BN[c.shape]);
+    f.tiles = SYMMETRIC ? f.tiles_a * (f.tiles_a + 1) / 2 : f.tiles_a * f.tiles_b;
+    f.slices /= KIND == HIGH ? 2 : 1;
+    f.slices_per_split = c.per;
+    const int64_t all = static_cast<int64_t>(f.tiles) * c.split;
+    const dim3 groups(static_cast<unsigned>(all));
+    if (c.shape == SHAPE_64 && all <= 256) {
+        hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Deep64, 1>), groups, dim3(Of::Deep64::NT), 0, st, f);
+    } else if (c.shape == SHAPE_64) {
+        hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Of64, 3>), groups, dim3(Of::Of64::NT), 0, st, f);
+    } else if (c.shape == SHAPE_128) {
+        hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Of128, 2>), groups, dim3(Of::Of128::NT), 0, st, f);
+    } else if (c.shape == SHAPE_256) {
+        hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Of256, 1>), groups, dim3(Of::Of256::NT), 0, st, f);
+    } else if constexpr (!SYMMETRIC) {
+        if (c.shape == SHAPE_192)
+            hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Of192, 1>), groups, dim3(Of::Of192::NT), 0, st, f);
+        else
+            hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Of160, 1>), groups, dim3(Of::Of160::NT), 0, st, f);
+    }
+}
+// A A's polynomial or X X^T, whole or in shares.
+template <Mode MODE> void launch_symmetric(Product f, const Choice &c, hipStream_t st) {
+    if (c.split == 1) return c.high ? launch_product<MODE, float, HIGH>(f, c, st) : launch_product<MODE, float, PAIRS>(f, c, st);
+    c.high ? launch_product<SHARE, float, HIGH>(f, c, st) : launch_product<SHARE, float, PAIRS>(f, c, st);
+    const int side = SHAPE_BM[c.shape], along = static_cast<int>((f.rows_a + side - 1) / side);
+    f.tiles = along * (along + 1) / 2;
+    hipLaunchKernelGGL(k_muon_join<MODE>, dim3(static_cast<unsigned>(f.tiles * (side / 64) * (side / 64))), dim3(256), 0, st, f, c.split, side);
+}
+size_t shares_bytes(const Choice &c, int64_t rows) {
+    const size_t side = static_cast<size_t>(SHAPE_BM[c.shape]), along = (static_cast<size_t>(rows) + side - 1) / side;
+    return c.split == 1 ? 0 : static_cast<size_t>(c.split) * (along * (along + 1) / 2) * side * side * sizeof(float);
 }
 
-constexpr int64_t MAX_SIDE = 1 << 16, MAX_STEPS = 64;
+constexpr int64_t MAX_SIDE = 1 << 16, MAX_STEPS = 64, COARSE_FROM = 256;
 bool update_ok(int64_t rows, int64_t cols) { return rows >= 0 && cols >= 0 && rows <= MAX_SIDE && cols <= MAX_SIDE && rows * cols < (static_cast<int64_t>(1) << 31); }
 
 // The workspace: X and, twice, X transposed; A, B; partial sums.
 struct Workspace {
     size_t x, xt[2], gram, poly, squares, shares, bytes;
-    Choice for_gram;
+    Choice gram_of[2], poly_of[2];  // of the pairs, of their h alone
 };
 Workspace workspace_of(int64_t less, int64_t more) {
     Workspace w{};
@@ -365,8 +507,14 @@ Workspace workspace_of(int64_t less, int64_t more) {
     w.gram = take(pairs_bytes(less, less));
     w.poly = take(pairs_bytes(less, less));
     w.squares = take(MIX_GROUPS * sizeof(double));
-    w.for_gram = choice_of(less, less, more, true, true);
-    w.shares = take(w.for_gram.split == 1 ? 0 : static_cast<size_t>(w.for_gram.split) * static_cast<size_t>(less) * static_cast<size_t>(less) * sizeof(float));
+    size_t most = 0;
+    for (int high = 0; high < 2; ++high) {
+        w.gram_of[high] = choice_of(less, less, more, true, false, high != 0);
+        w.poly_of[high] = choice_of(less, less, less, true, false, high != 0);
+        for (const Choice &c : {w.gram_of[high], w.poly_of[high]})
+            if (const size_t bytes = shares_bytes(c, less); bytes > most) most = bytes;
+    }
+    w.shares = take(most);
     w.bytes = at;
     return w;
 }
@@ -409,35 +557,38 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
     });
 
     const int along = static_cast<int>(padded(more) / 32), side = static_cast<int>(padded(less) / 32);
-    const int poly_tile = choice_of(less, less, less, true, false).side, next_tile = choice_of(less, more, less, false, false).side;
+    // Where w is of 16 bits: products of 11 bits in all steps but the last ones, and in bf16's last.
+    const bool coarser = dt != ADATOPK_F32 && less >= COARSE_FROM, coarse_end = coarser && dt == ADATOPK_BF16;
+    const int fine = !coarser ? steps : dt == ADATOPK_F16 ? 3 : 2;
+    const Choice next = choice_of(less, more, less, false, true, false), next_coarse = choice_of(less, more, less, false, true, true);
+    const Choice last = choice_of(cols, rows, less, false, false, coarse_end);
     for (int step = 0; step < steps; ++step) {
+        const bool high = steps - step > fine || (coarse_end && step + 1 == steps);
         Product p{};
+        p.partial = reinterpret_cast<float *>(base + at.shares);
         p.a = p.b = x;
         p.rows_a = p.rows_b = less;
         p.slices = along;
-        p.slices_per_split = at.for_gram.per;
         p.by_j = p.by_i = gram;
-        if (at.for_gram.split == 1) {
-            launch_product<GRAM, float>(p, at.for_gram.side, 1, st);
-        } else {
-            p.partial = reinterpret_cast<float *>(base + at.shares);
-            launch_product<SHARE, float>(p, at.for_gram.side, at.for_gram.split, st);
-            const int64_t row_octets = padded(less) / 8;
-            const uint32_t all = static_cast<uint32_t>(less * row_octets);
-            hipLaunchKernelGGL(k_muon_join, dim3((all + 255) / 256), dim3(256), 0, st, p.partial, at.for_gram.split, less, gram,
-                               Divisor(static_cast<uint32_t>(row_octets)), all);
-        }
+        launch_symmetric<GRAM>(p, at.gram_of[high], st);
         p.a = p.b = p.gram = gram;
-        p.slices = p.slices_per_split = side;
+        p.slices = side;
         p.by_j = p.by_i = poly;
-        launch_product<POLY, float>(p, poly_tile, 1, st);
+        const bool coarse = high && step + 1 < steps;
+        p.diagonal = coarse ? 0.f : NS_A;
+        launch_symmetric<POLY>(p, at.poly_of[high], st);
         if (step + 1 < steps) {
             p.a = poly;
             p.b = xt;
             p.rows_b = more;
             p.by_j = xt_next;
             p.by_i = x;
-            launch_product<NEXT, float>(p, next_tile, 1, st);
+            p.old_by_j = xt;
+            p.old_by_i = x;
+            if (coarse)
+                launch_product<NEXT, float, HIGH>(p, next_coarse, st);
+            else
+                launch_product<NEXT, float, PAIRS>(p, next, st);
             const Pairs t = xt;
             xt = xt_next;
             xt_next = t;
@@ -452,7 +603,10 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
             p.decay = decay;
             with_type(dt, [&](auto *null) {
                 using T = std::remove_pointer_t<decltype(null)>;
-                launch_product<LAST, T>(p, next_tile, 1, st);
+                if constexpr (__is_same(T, Bf16)) {
+                    if (coarse_end) return launch_product<LAST, T, HIGH>(p, last, st);
+                }
+                launch_product<LAST, T, PAIRS>(p, last, st);
             });
         }
     }
