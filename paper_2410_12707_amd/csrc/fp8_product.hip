@@ -251,30 +251,45 @@ template <typename T, int TJ> __global__ __launch_bounds__(FEW_WAVES * 64) void 
     }
 }
 
-enum Form { LARGE, MIDDLE, SMALL, FEW, NONE };
-constexpr int SIDE[] = {256, 128, 64};
+enum Form { LARGE, MIDDLE, SMALL, DEEP, TILED, FEW = TILED, NONE };
+template <Kind KIND> struct Tiles {
+    using Large = RowTile<KIND, 256, 256, 2, 4, 2>;
+    using Middle = RowTile<KIND, 128, 128, 2, 2, 2>;
+    using Small = RowTile<KIND, 64, 64, 2, 2, 2>;
+    using Deep = RowTile<KIND, 64, 64, 1, 1, 2, 4>;
+};
+constexpr int SIDE[TILED] = {256, 128, 64, 64}, SLOTS[TILED] = {256, 512, 1024, 256};  // of the chip
 
 struct Cut {
     Form form;
     int tiles_out, tiles_rows, slices, split, per;
 };
-constexpr int64_t FEW_ROWS = 64;
+// us: of a slice of 128 for a workgroup with a few others on the chip and on a full one, and what a workgroup takes beside; by the 8-bit instruction, and as bf16 for fp32
+// results.  Measured at 14 sizes, 65 x 768 x 768 to 16384 x 1600 x 6400: by tile 193, 216, 302, 550 us there, 57, 69, 115, 140 for 4096 x 4096 x 4096, 17, 8.6, 6.0, 6.4
+// for 1024 x 1024 x 1024, 57, 24, 17, 11 for 128 x 6400 x 1600.
+constexpr double STEP_ALONE[2][TILED] = {{1.0, 0.38, 0.25, 0.125}, {1.95, 0.66, 0.38, 0.2}}, STEP_FULL[2][TILED] = {{1.5, 0.88, 0.69, 0.16}, {3.1, 1.7, 1.1, 0.26}};
+constexpr double BESIDE[2][TILED] = {{8., 6., 4.8, 5.}, {10., 8., 5.5, 5.3}};
+// Up to so many tokens k_fp8_few is as quick or quicker: 16 tokens, 1600 x 6400, 5.3 us against 6.6, 32 tokens, 6400 x 1600, 10.9 against 12.2; 48, 1600 x 6400, 10.5
+// against 7.0.
+constexpr int64_t FEW_ROWS = 32;
 constexpr int SPLIT_MAX = 16;
-Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in) {
+Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in, bool exact) {
     const int slices = static_cast<int>(adatopk_internal::fp8_pitch(n_in) / SLICE);
     Cut best{FEW, 0, 0, slices, 1, slices};
     if (slices == 0) best.form = NONE;  // (nothing to add up: what the join adds to no shares)
     if (rows <= FEW_ROWS || slices == 0) return best;
     double least = 0;
-    for (int t = 0; t < 3; ++t) {
+    for (int t = 0; t < TILED; ++t) {
         const int64_t out = (n_out + SIDE[t] - 1) / SIDE[t], along = (rows + SIDE[t] - 1) / SIDE[t], tiles = out * along;
-        const int units = t == LARGE ? 256 : t == MIDDLE ? 512 : 1024;
-        const double step = t == LARGE ? 1.1 : t == MIDDLE ? 0.6 : 0.35, beside = t == LARGE ? 8. : t == MIDDLE ? 5. : 4.;
         for (int split = 1; split <= SPLIT_MAX && split <= slices; ++split) {
             const int per = (slices + split - 1) / split;
             if ((slices + per - 1) / per != split) continue;
-            const double rounds = static_cast<double>((tiles * split + units - 1) / units);
-            const double cost = rounds * (beside + step * per) + (split == 1 ? 0. : 5. + 0.4e-6 * 4. * split * static_cast<double>(rows) * static_cast<double>(n_out));
+            const double filled = static_cast<double>(tiles * split) / SLOTS[t], some = filled < 1. ? filled : 1.;
+            // workgroups that share a compute unit do not end together: their rounds run into one another
+            const double rounds = filled <= 1. ? 1. : SLOTS[t] > 256 ? filled : static_cast<double>((tiles * split + 255) / 256);
+            const double step = STEP_ALONE[exact][t] + some * (STEP_FULL[exact][t] - STEP_ALONE[exact][t]);
+            const double join = split == 1 ? 0. : 4.5 + 0.4e-6 * 4. * split * static_cast<double>(rows) * static_cast<double>(n_out);
+            const double cost = rounds * (BESIDE[exact][t] + step * per) + join;
             if (best.form == FEW || cost < least) {
                 least = cost;
                 best = Cut{static_cast<Form>(t), static_cast<int>(out), static_cast<int>(along), slices, split, per};
@@ -282,6 +297,9 @@ Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in) {
         }
     }
     return best;
+}
+size_t shares_bytes(const Cut &c, int64_t rows, int64_t n_out) {
+    return c.split == 1 ? 0 : align_up(static_cast<size_t>(c.split) * static_cast<size_t>(rows) * static_cast<size_t>(n_out) * sizeof(float), 256);
 }
 
 constexpr int64_t MAX_FEATURES = 1 << 17;
@@ -296,8 +314,8 @@ extern "C" {
 
 size_t adatopk_fp8_product_workspace_bytes(int64_t rows, int64_t n_out, int64_t n_in) {
     if (!product_ok(rows, n_out, n_in) || rows == 0 || n_out == 0) return 0;
-    const Cut c = cut_of(rows, n_out, n_in);
-    return c.split == 1 ? 0 : align_up(static_cast<size_t>(c.split) * static_cast<size_t>(rows) * static_cast<size_t>(n_out) * sizeof(float), 256);
+    const size_t one = shares_bytes(cut_of(rows, n_out, n_in, false), rows, n_out), other = shares_bytes(cut_of(rows, n_out, n_in, true), rows, n_out);
+    return one > other ? one : other;
 }
 
 adatopk_status adatopk_fp8_product(const void *fp8_x, const void *fp8_w, int64_t rows, int64_t n_out, int64_t n_in, const void *bias, adatopk_dtype bias_dt,
@@ -308,11 +326,10 @@ adatopk_status adatopk_fp8_product(const void *fp8_x, const void *fp8_w, int64_t
     if (!matrix_ok(y, y_stride, rows, n_out, dt) || !pointer_ok_or_null(bias, static_cast<size_t>(elem_size(bias_dt))) ||
         (add != nullptr && !matrix_ok(add, add_stride, rows, n_out, dt)) || (n_in > 0 && (!pointer_ok(fp8_x, 16) || !pointer_ok(fp8_w, 16))))
         return ADATOPK_EINVAL;
-    const Cut c = cut_of(rows, n_out, n_in);
-    if (c.split > 1) {
-        if (!pointer_ok(workspace, 256)) return ADATOPK_EINVAL;
-        if (workspace_bytes < adatopk_fp8_product_workspace_bytes(rows, n_out, n_in)) return ADATOPK_EWORKSPACE;
-    }
+    const size_t need = adatopk_fp8_product_workspace_bytes(rows, n_out, n_in);
+    if (need > 0 && !pointer_ok(workspace, 256)) return ADATOPK_EINVAL;
+    if (workspace_bytes < need) return ADATOPK_EWORKSPACE;
+    const Cut c = cut_of(rows, n_out, n_in, dt == ADATOPK_F32);
     const Product f{fp8_of(const_cast<void *>(fp8_x), rows, n_in), fp8_of(const_cast<void *>(fp8_w), n_out, n_in), rows, n_out, c.slices, c.split, c.per, c.tiles_out,
                     c.tiles_rows, bias, add, bias_dt != dt, add_stride, y_stride, y, static_cast<float *>(workspace)};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -328,24 +345,19 @@ adatopk_status adatopk_fp8_product(const void *fp8_x, const void *fp8_w, int64_t
         if (c.form == NONE) return join(0);
         if (c.form == FEW) {
             const dim3 groups(static_cast<unsigned>((n_out + 15) / 16)), threads(FEW_WAVES * 64);
-            const auto kernel = rows <= 16 ? k_fp8_few<T, 1> : rows <= 32 ? k_fp8_few<T, 2> : k_fp8_few<T, 4>;
-            hipLaunchKernelGGL(kernel, groups, threads, 0, st, f);
+            hipLaunchKernelGGL((rows <= 16 ? k_fp8_few<T, 1> : k_fp8_few<T, 2>), groups, threads, 0, st, f);
             return;
         }
-        constexpr Kind KIND = sizeof(T) == 4 ? FP8_EXACT : FP8_FAST;
-        using Large = RowTile<KIND, 256, 256, 2, 4, 2>;
-        using Middle = RowTile<KIND, 128, 128, 2, 2, 2>;
-        using Small = RowTile<KIND, 64, 64, 2, 2, 2>;
-        using Deep = RowTile<KIND, 64, 64, 1, 1, 2, 4>;
+        using Of = Tiles<sizeof(T) == 4 ? FP8_EXACT : FP8_FAST>;
         const dim3 groups(static_cast<unsigned>(c.tiles_out * c.tiles_rows * c.split));
-        if (c.form == SMALL && groups.x <= 256)
-            hipLaunchKernelGGL((k_fp8_product<T, Deep, 1>), groups, dim3(Deep::NT), 0, st, f);
-        else if (c.form == LARGE)
-            hipLaunchKernelGGL((k_fp8_product<T, Large, 1>), groups, dim3(Large::NT), 0, st, f);
+        if (c.form == LARGE)
+            hipLaunchKernelGGL((k_fp8_product<T, typename Of::Large, 1>), groups, dim3(Of::Large::NT), 0, st, f);
         else if (c.form == MIDDLE)
-            hipLaunchKernelGGL((k_fp8_product<T, Middle, 2>), groups, dim3(Middle::NT), 0, st, f);
+            hipLaunchKernelGGL((k_fp8_product<T, typename Of::Middle, 2>), groups, dim3(Of::Middle::NT), 0, st, f);
+        else if (c.form == SMALL)
+            hipLaunchKernelGGL((k_fp8_product<T, typename Of::Small, 4>), groups, dim3(Of::Small::NT), 0, st, f);
         else
-            hipLaunchKernelGGL((k_fp8_product<T, Small, 4>), groups, dim3(Small::NT), 0, st, f);
+            hipLaunchKernelGGL((k_fp8_product<T, typename Of::Deep, 1>), groups, dim3(Of::Deep::NT), 0, st, f);
         if (c.split > 1) join(c.split);
     });
     return launched();
