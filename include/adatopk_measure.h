@@ -64,9 +64,15 @@ size_t adatopk_measure_workspace_offset(int32_t what, int64_t n_total, int32_t n
  *   layernorm    out[0]          lanes to a row                 out[1]  octets of a row to a lane
  *                out[2]          rows under way at a time
  *                out[3]          backward pass with the weight's gradient: 0 if that is added up along with the rows, otherwise the number of
- *                                shares of the rows in which it is, apart from them */
+ *                                shares of the rows in which it is, apart from them
+ *   fp8_product  out[0]          side of a tile, 0: a few tokens     out[1]  1: the tile's wavefronts take turns along the sum
+ *                out[2]          shares of the sum; more than one are joined by a second kernel
+ *   muon_update  eight products, three numbers each (sides of a tile, and what out[2] is above, + 64 where its wavefronts take turns along the sum): X X^T, A A,
+ *                B X and the last step's B X, which writes w, from pairs, then from their h alone */
 adatopk_status adatopk_measure_weight_grad_cut(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, int64_t dy_stride, int32_t *out);
 adatopk_status adatopk_measure_layernorm_cut(int64_t rows, int64_t cols, int32_t backward, int32_t *out);
+adatopk_status adatopk_measure_fp8_product_cut(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, int32_t *out);
+adatopk_status adatopk_measure_muon_update_cut(int64_t rows, int64_t cols, int32_t *out);
 
 /* Plain streaming kernels on `hip_stream`; all pointers are device memory, 16-byte
  * aligned; bytes must be a multiple of 16.

@@ -74,6 +74,10 @@ def load_measure_library() -> ctypes.CDLL:
     lib.adatopk_measure_weight_grad_cut.restype = i32
     lib.adatopk_measure_layernorm_cut.argtypes = [ctypes.c_int64, ctypes.c_int64, i32, p]
     lib.adatopk_measure_layernorm_cut.restype = i32
+    lib.adatopk_measure_fp8_product_cut.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, i32, p]
+    lib.adatopk_measure_fp8_product_cut.restype = i32
+    lib.adatopk_measure_muon_update_cut.argtypes = [ctypes.c_int64, ctypes.c_int64, p]
+    lib.adatopk_measure_muon_update_cut.restype = i32
     lib.adatopk_measure_copy.argtypes = [p, p, sz, p]
     lib.adatopk_measure_copy.restype = i32
     lib.adatopk_measure_read_only.argtypes = [p, sz, p, p]
@@ -887,6 +891,21 @@ def measure_layernorm_cut(rows: int, cols: int, backward: bool):
     out = (ctypes.c_int32 * 4)()
     _check(load_measure_library().adatopk_measure_layernorm_cut(int(rows), int(cols), 1 if backward else 0, out), "adatopk_measure_layernorm_cut")
     return tuple(out)
+
+
+def measure_fp8_product_cut(rows: int, n_out: int, n_in: int, dtype: torch.dtype):
+    """(side of a tile or 0 for a few tokens, whether its wavefronts take turns along the sum, shares of the sum) of a product."""
+    out = (ctypes.c_int32 * 3)()
+    _check(load_measure_library().adatopk_measure_fp8_product_cut(int(rows), int(n_out), int(n_in), _dtype_code(dtype), out), "adatopk_measure_fp8_product_cut")
+    return out[0], bool(out[1]), out[2]
+
+
+def measure_muon_update_cut(rows: int, cols: int):
+    """((sides of a tile, whether its wavefronts take turns along the sum, shares of the sum)) of an update's eight products: X X^T, the
+    polynomial, X's next step and the change of w, from pairs and from the coarse steps' halves."""
+    out = (ctypes.c_int32 * 24)()
+    _check(load_measure_library().adatopk_measure_muon_update_cut(int(rows), int(cols), out), "adatopk_measure_muon_update_cut")
+    return tuple(((out[3 * i], out[3 * i + 1]), out[3 * i + 2] >= 64, out[3 * i + 2] % 64) for i in range(8))
 
 
 def measure_copy(dst: torch.Tensor, src: torch.Tensor) -> None:

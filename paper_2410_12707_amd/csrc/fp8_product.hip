@@ -363,4 +363,15 @@ adatopk_status adatopk_fp8_product(const void *fp8_x, const void *fp8_w, int64_t
     return launched();
 }
 
+#ifdef ADATOPK_MEASURE_BUILD
+adatopk_status adatopk_measure_fp8_product_cut(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, int32_t *out) {
+    if (!dtype_ok(dt) || !product_ok(rows, n_out, n_in) || rows == 0 || n_out == 0 || n_in == 0) return ADATOPK_EINVAL;
+    const Cut c = cut_of(rows, n_out, n_in, dt == ADATOPK_F32);
+    out[0] = c.form == FEW ? 0 : SIDE[c.form];
+    out[1] = c.form == DEEP ? 1 : 0;
+    out[2] = c.split;
+    return ADATOPK_OK;
+}
+#endif
+
 }  // extern "C"

@@ -18,6 +18,9 @@
 // 1.4e-3 and 4.3e-3 at the worst of eight) and products are not what takes the time: there all steps take the full 22 bits.
 #include <hip/hip_runtime.h>
 
+#ifdef ADATOPK_MEASURE_BUILD
+#include "adatopk_measure.h"
+#endif
 #include "row_tiles.h"
 
 // Products and sums are fused where the code says so and nowhere else.
@@ -414,12 +417,15 @@ Choice choice_of(int64_t rows_a, int64_t rows_b, int64_t sum, bool symmetric, bo
     for (int t = 0; t < SHAPES; ++t)
         for (int turned = 0; turned < (may_turn && SHAPE_BM[t] != SHAPE_BN[t] ? 2 : 1); ++turned) {
             if (symmetric && SHAPE_BM[t] != SHAPE_BN[t]) continue;
+            // X's tiles have to reach to the end of its last 64, whose zeros they write
+            if (may_turn && padded(turned ? rows_b : rows_a) > ((turned ? rows_b : rows_a) + SHAPE_BM[t] - 1) / SHAPE_BM[t] * SHAPE_BM[t]) continue;
             const int64_t a = ((turned ? rows_b : rows_a) + SHAPE_BM[t] - 1) / SHAPE_BM[t], b = ((turned ? rows_a : rows_b) + SHAPE_BN[t] - 1) / SHAPE_BN[t];
             for (int split = 1; split <= (symmetric ? SPLIT_MAX : 1) && split <= slices; ++split) {
                 const int per = (slices + split - 1) / split;
                 if ((slices + per - 1) / per != split) continue;
                 const int64_t tiles = (symmetric ? a * (a + 1) / 2 : a * b) * split;
                 const bool deep = t == SHAPE_64 && tiles <= 256;
+                if (symmetric && high && t == SHAPE_64 && split == 1 && !deep) continue;  // never the least over the sizes that there are: no kernel
                 const double filled = static_cast<double>(tiles) / SHAPE_SLOTS[t];
                 // workgroups that share a compute unit slow one another down, and their rounds run into one another
                 const bool shared = SHAPE_SLOTS[t] > 256;
@@ -460,7 +466,8 @@ template <Mode MODE, typename T, Kind KIND> void launch_product(Product f, const
     if (c.shape == SHAPE_64 && all <= 256) {
         hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Deep64, 1>), groups, dim3(Of::Deep64::NT), 0, st, f);
     } else if (c.shape == SHAPE_64) {
-        hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Of64, 3>), groups, dim3(Of::Of64::NT), 0, st, f);
+        if constexpr (KIND != HIGH || (MODE != GRAM && MODE != POLY))
+            hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Of64, 3>), groups, dim3(Of::Of64::NT), 0, st, f);
     } else if (c.shape == SHAPE_128) {
         hipLaunchKernelGGL((k_muon_product<MODE, T, typename Of::Of128, 2>), groups, dim3(Of::Of128::NT), 0, st, f);
     } else if (c.shape == SHAPE_256) {
@@ -612,5 +619,27 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
     }
     return launched();
 }
+
+#ifdef ADATOPK_MEASURE_BUILD
+adatopk_status adatopk_measure_muon_update_cut(int64_t rows, int64_t cols, int32_t *out) {
+    if (!update_ok(rows, cols) || rows == 0 || cols == 0) return ADATOPK_EINVAL;
+    const int64_t less = rows < cols ? rows : cols, more = rows < cols ? cols : rows;
+    for (int high = 0; high < 2; ++high) {
+        const Choice four[] = {choice_of(less, less, more, true, false, high != 0), choice_of(less, less, less, true, false, high != 0),
+                               choice_of(less, more, less, false, true, high != 0), choice_of(cols, rows, less, false, false, high != 0)};
+        for (int k = 0; k < 4; ++k) {
+            const Choice &c = four[k];
+            const int64_t ra = k < 2 ? less : k == 3 ? cols : c.turned ? more : less, rb = k < 2 ? less : k == 3 ? rows : c.turned ? less : more;
+            const int64_t a = (ra + SHAPE_BM[c.shape] - 1) / SHAPE_BM[c.shape], b = (rb + SHAPE_BN[c.shape] - 1) / SHAPE_BN[c.shape];
+            const bool deep = c.shape == SHAPE_64 && (k < 2 ? a * (a + 1) / 2 : a * b) * c.split <= 256;
+            int32_t *const to = out + (high * 4 + k) * 3;
+            to[0] = SHAPE_BM[c.shape];
+            to[1] = SHAPE_BN[c.shape];
+            to[2] = c.split + (deep ? 64 : 0);
+        }
+    }
+    return ADATOPK_OK;
+}
+#endif
 
 }  // extern "C"

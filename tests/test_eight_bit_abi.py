@@ -1,0 +1,175 @@
+"""Refusals, sizes and forms of the calls around projections in 8-bit floating point; no GPU needed: every refused call returns before it touches the device."""
+import numpy as np
+import pytest
+import torch
+
+import eight_bit_forms as forms
+import fp8_reference as fp8
+from paper_2410_12707_amd import binding as B
+
+OK, EINVAL, EWORKSPACE = 0, 1, 2
+P, WS = 0x10000, 0x100000  # never dereferenced
+F32, BF16, F16 = 0, 1, 2
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return B.load_library()
+
+
+def test_the_reference_rounds_as_the_type_does():
+    x = torch.cat([torch.randn(4000) * 2.0 ** torch.randint(-12, 9, (4000,)), torch.from_numpy(np.concatenate([fp8.TABLE, fp8.MIDDLES, -fp8.MIDDLES])).float()]).clamp(-448, 448)
+    assert np.array_equal(fp8.bytes_of(x.double().numpy()), x.to(torch.float8_e4m3fn).view(torch.uint8).numpy())
+    assert np.array_equal(fp8.TABLE, torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy())
+
+
+def test_fp8_bytes(lib):
+    for rows, cols in ((1, 1), (1, 128), (3, 129), (257, 1600), (16384, 6400), (0, 5), (5, 0)):
+        assert B.adatopk_fp8_bytes(rows, cols) == (fp8.fp8_layout(rows, cols)[3] if rows * cols else 0), (rows, cols)
+    assert B.adatopk_fp8_bytes(-1, 5) == 0 and B.adatopk_fp8_bytes(5, -1) == 0
+    assert B.adatopk_fp8_bytes(1 << 27, 128) == 0           # 2^34 elements
+    assert B.adatopk_fp8_bytes((1 << 27) - 1, 128) > 1 << 33  # one row less
+    assert B.adatopk_fp8_bytes(1, (1 << 31) - 1) == 0
+
+
+def test_fp8_calls_refuse(lib):
+    s, d, w = lib.adatopk_fp8_store, lib.adatopk_fp8_load, lib.adatopk_fp8_store_weight
+    for bad in ((P, 64, 4, 64, 3, P), (P, 64, -1, 64, F32, P), (P, 64, 4, -1, F32, P), (P, 63, 4, 64, F32, P), (P, -64, 4, 64, F32, P), (None, 64, 4, 64, F32, P),
+                (P + 2, 64, 4, 64, F32, P), (P + 1, 64, 4, 64, BF16, P), (P, 64, 4, 64, F32, None), (P, 64, 4, 64, F32, P + 8), (P, 128, 1 << 27, 128, F32, P)):
+        assert s(*bad, None) == EINVAL, bad
+    assert s(None, 0, 0, 64, F32, None, None) == OK and s(None, 0, 4, 0, F32, None, None) == OK
+    for bad in ((P, 4, 64, 9, P, 64), (P, 4, 64, F32, P, 63), (P, 4, 64, F32, None, 64), (None, 4, 64, F32, P, 64), (P + 4, 4, 64, F32, P, 64), (P, 4, 64, F16, P + 1, 64)):
+        assert d(*bad, None) == EINVAL, bad
+    assert d(None, 0, 64, F32, None, 0, None) == OK
+    for bad in ((P, 64, 4, 64, 3, P, P), (P, 63, 4, 64, F32, P, P), (None, 64, 4, 64, F32, P, P), (P, 64, 4, 64, F32, None, None), (P, 64, 4, 64, F32, P + 8, None),
+                (P, 64, 4, 64, F32, P, P + 4), (P, 64, -4, 64, F32, P, P)):
+        assert w(*bad, None) == EINVAL, bad
+    assert w(None, 0, 0, 64, F32, None, None, None) == OK
+
+
+def test_fp8_product_refuses(lib):
+    names = ["x", "w", "rows", "no", "ni", "bias", "bdt", "add", "as", "y", "ys", "dt", "ws", "bytes", "st"]
+    assert lib.adatopk_fp8_product_workspace_bytes(512, 768, 768) == 0
+    need = lib.adatopk_fp8_product_workspace_bytes(35, 70, 5256)
+    assert need >= 2 * 35 * 70 * 4
+    for bad in ((-1, 48, 64), (100, -1, 64), (100, 48, -1), (100, 131073, 64), (100, 48, 131073), (1 << 31, 48, 64), (0, 48, 64), (100, 0, 64)):
+        assert lib.adatopk_fp8_product_workspace_bytes(*bad) == 0, bad
+    good = dict(zip(names, [P, P, 35, 70, 5256, P, F32, P, 70, P, 70, F32, WS, need, None]))
+
+    def f(**kw):
+        return lib.adatopk_fp8_product(*(dict(good, **kw)[k] for k in names))
+
+    for bad in (dict(dt=3), dict(bdt=BF16), dict(bdt=7), dict(rows=-1), dict(no=-1), dict(ni=-1), dict(no=131073, ys=131073), dict(ni=131073), dict(rows=1 << 31), dict(x=None),
+                dict(w=None), dict(x=P + 8), dict(w=P + 8), dict(y=None), dict(y=P + 2), dict(ys=69), dict(bias=P + 2), dict(add=P + 1), dict(**{"as": 69}), dict(ws=None),
+                dict(ws=WS + 64)):
+        assert f(**bad) == EINVAL, bad
+    assert f(bytes=need - 1) == EWORKSPACE
+    assert f(rows=0, x=None, y=None) == OK and f(no=0, w=None, y=None) == OK
+
+
+def test_rmsnorm_calls_refuse(lib):
+    names = ["x", "xs", "res", "rs", "w", "wdt", "rows", "cols", "dt", "eps", "sum", "ss", "y", "ys", "rstd", "act8", "fp8", "st"]
+    good = dict(zip(names, [P, 64, None, 0, P, F32, 4, 64, F32, 1e-5, None, 0, P, 64, P, None, None, None]))
+
+    def f(**kw):
+        return lib.adatopk_rmsnorm_forward(*(dict(good, **kw)[k] for k in names))
+
+    for bad in (dict(dt=4), dict(rows=-1), dict(cols=-1), dict(cols=32769, xs=32769, ys=32769), dict(xs=63), dict(ys=63), dict(x=None), dict(y=None), dict(x=P + 2),
+                dict(y=None, act8=P), dict(eps=-1.0), dict(eps=float("nan")), dict(wdt=BF16), dict(w=P + 2), dict(res=P, rs=5), dict(sum=P, ss=64), dict(res=P, rs=64, sum=P, ss=3),
+                dict(rstd=P + 1), dict(act8=P + 8), dict(fp8=P + 8), dict(wdt=9)):
+        assert f(**bad) == EINVAL, bad
+    assert f(rows=0, x=None, y=None) == OK
+
+    names_b = ["dy", "dys", "x", "xs", "act8", "rstd", "w", "wdt", "dsum", "dss", "rows", "cols", "dt", "dx", "dxs", "dw", "acc", "ws", "bytes", "st"]
+    need = lib.adatopk_rmsnorm_backward_workspace_bytes(4, 64)
+    assert need >= 64 * 4 and lib.adatopk_rmsnorm_backward_workspace_bytes(4, 32769) == 0 and lib.adatopk_rmsnorm_backward_workspace_bytes(-1, 4) == 0
+    good_b = dict(zip(names_b, [P, 64, P, 64, None, P, P, F32, None, 0, 4, 64, F32, P, 64, P, 0, WS, need, None]))
+
+    def b(**kw):
+        return lib.adatopk_rmsnorm_backward(*(dict(good_b, **kw)[k] for k in names_b))
+
+    for bad in (dict(dt=4), dict(rows=-1), dict(cols=40000, dys=40000, xs=40000, dxs=40000), dict(dys=63), dict(xs=63), dict(dxs=63), dict(dy=None), dict(dx=None), dict(x=None),
+                dict(act8=P), dict(x=None, act8=P + 8), dict(rstd=None), dict(wdt=F16), dict(w=P + 2), dict(dsum=P, dss=1), dict(dw=P + 2), dict(ws=None), dict(ws=WS + 16)):
+        assert b(**bad) == EINVAL, bad
+    assert b(bytes=need - 1) == EWORKSPACE
+
+
+def test_muon_update_refuses(lib):
+    names = ["g", "gs", "gdt", "m", "mu", "nesterov", "rows", "cols", "steps", "eps", "w", "ws_", "dt", "scale", "decay", "ws", "bytes", "st"]
+    need = lib.adatopk_muon_update_workspace_bytes(48, 64)
+    assert need > 48 * 64 * 4 * 3
+    for bad in ((-1, 64), (48, -1), (65537, 64), (48, 65537), (0, 64), (65536, 65536)):
+        assert lib.adatopk_muon_update_workspace_bytes(*bad) == 0, bad
+    good = dict(zip(names, [P, 64, F32, P, 0.9, 1, 48, 64, 5, 1e-7, P, 64, BF16, -0.1, 0.9, WS, need, None]))
+
+    def f(**kw):
+        return lib.adatopk_muon_update(*(dict(good, **kw)[k] for k in names))
+
+    for bad in (dict(gdt=3), dict(dt=3), dict(rows=-1), dict(cols=65537, gs=65537, ws_=65537), dict(steps=0), dict(steps=65), dict(eps=-1.0), dict(eps=float("nan")), dict(g=None),
+                dict(g=P + 2), dict(gs=63), dict(w=None), dict(w=P + 1), dict(ws_=63), dict(m=P + 2), dict(ws=None), dict(ws=WS + 16)):
+        assert f(**bad) == EINVAL, bad
+    assert f(bytes=need - 1) == EWORKSPACE
+    assert f(rows=0, g=None, w=None) == OK
+
+
+class Fake:
+    """What the binding looks at in a tensor on the device, from one in host memory."""
+
+    is_cuda = True
+
+    def __init__(self, t):
+        self.shape, self.dtype, self._t = t.shape, t.dtype, t
+
+    def __getattr__(self, name):
+        return getattr(self._t, name)
+
+
+def test_the_binding_refuses(monkeypatch):
+    monkeypatch.setattr(B, "_marshal", False)
+    monkeypatch.setattr(B, "_stream", lambda: None)
+    x, small, w = Fake(torch.zeros(4, 64)), Fake(torch.zeros(100, dtype=torch.uint8)), Fake(torch.zeros(48, 64))
+    for call, said in ((lambda: B.adatopk_fp8_store(x, small), "fp8 must be uint8"), (lambda: B.adatopk_fp8_load(small, x), "fp8 must be uint8"),
+                       (lambda: B.adatopk_fp8_store_weight(x, None, small), "fp8_transposed must be uint8"), (lambda: B.adatopk_fp8_product(small, small, 64, x, None), "fp8_x must be"),
+                       (lambda: B.adatopk_rmsnorm_forward(x, None, 1e-5, w, None), "y must be"), (lambda: B.adatopk_rmsnorm_forward(x, None, 1e-5, x, None, fp8=small), "fp8 must be"),
+                       (lambda: B.adatopk_rmsnorm_backward(x, x, None, Fake(torch.zeros(3)), None, x, None, None), "rstd must be"),
+                       (lambda: B.adatopk_muon_update(x, None, 0.0, False, w, 1.0, 0.0, small), "grad must have"),
+                       (lambda: B.adatopk_muon_update(w, Fake(torch.zeros(5)), 0.0, False, w, 1.0, 0.0, small), "momentum must be"),
+                       (lambda: B.adatopk_fp8_store(torch.zeros(4, 64), small), "device tensors")):
+        with pytest.raises(ValueError, match=said):
+            call()
+    with pytest.raises(TypeError):
+        B.adatopk_fp8_store(Fake(torch.zeros(4, 64, dtype=torch.float64)), Fake(torch.zeros(4096, dtype=torch.uint8)))
+
+
+def test_sizes_for_every_form_take_the_form_they_are_meant_for():
+    for dtype, form, size in forms.PRODUCTS:
+        side, along, split = B.measure_fp8_product_cut(*size, dtype)
+        assert (side, along, split > 1) == form, (dtype, size, side, along, split)
+    for which, tile, along, shared, size in forms.UPDATES:
+        cut = B.measure_muon_update_cut(*size)[which]
+        assert (cut[0], cut[1], cut[2] > 1) == (tile, along, shared), (which, size, cut)
+
+
+def test_there_is_no_other_form():
+    import random
+
+    rng = random.Random(3)
+
+    def size(most):
+        return max(1, int(round(most ** rng.random())))
+
+    known = {dtype: {form for d, form, _ in forms.PRODUCTS if d == dtype} for dtype in (forms.BF16, forms.F32)}
+    for _ in range(10000):
+        for dtype, table in known.items():
+            rows, n_out, n_in = size(70000), size(131072), size(131072)
+            side, along, split = B.measure_fp8_product_cut(rows, n_out, n_in, dtype)
+            assert (side, along, split > 1) in table, (rows, n_out, n_in, dtype)
+            assert split == 1 or B.adatopk_fp8_product_workspace_bytes(rows, n_out, n_in) >= split * rows * n_out * 4
+    table = {(which, tile, along, shared) for which, tile, along, shared, _ in forms.UPDATES}
+    for _ in range(10000):
+        rows, cols = size(65536), size(65536)
+        if rows * cols >= 1 << 31:
+            continue
+        for which, cut in enumerate(B.measure_muon_update_cut(rows, cols)):
+            if which < 4 or min(rows, cols) >= 256:  # below that no product is from the h alone
+                assert (which, cut[0], cut[1], cut[2] > 1) in table, (which, rows, cols, cut)
