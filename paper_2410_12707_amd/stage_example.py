@@ -1,6 +1,6 @@
 """A pipeline stage in training between two slow links: the feed-forward half of a transformer block.
 
-    python -m paper_2410_12707_amd.stage_example
+    python -m paper_2410_12707_amd.stage_example [--eight-bit]
 
 Activations come in and go out as compressed messages, gradients come back the same way (paper Sec. 3.3 and 5.1), and while several micro-batches
 are under way (Sec. 3.6) each one's activations wait in 8 bits:
@@ -10,8 +10,13 @@ are under way (Sec. 3.6) each one's activations wait in 8 bits:
                dx = layer norm's gradient + dout -> message
 
 The matrix products between activations and weights are torch's; everything else is this package's.
+
+With --eight-bit the norm is a root-mean-square norm and the projections, forward and backward, run in 8-bit floating point, from what the norm, GELU and the links
+hand over; behind the last micro-batch the weights are updated by their orthogonalised gradients and put into 8 bits again.  Every product is this package's then.
 """
 from __future__ import annotations
+
+import argparse
 
 import torch
 
@@ -63,6 +68,53 @@ class FeedForwardStage:
         return dx
 
 
+class EightBitStage(FeedForwardStage):
+    """The same with projections in 8-bit floating point, a root-mean-square norm before them and updates of their weights."""
+
+    def __init__(self, features: int, hidden: int, tokens: int, micro_batches: int, dtype=torch.bfloat16, seed: int = 0):
+        super().__init__(features, hidden, tokens, micro_batches, dtype, seed)
+        self.eight = {name: (B.new_fp8(*getattr(self, name).shape), B.new_fp8(*reversed(getattr(self, name).shape))) for name in ("w1", "w2")}
+        self.momentum = {name: torch.zeros_like(self.grad[name]) for name in self.eight}
+        need = max(B.adatopk_rmsnorm_backward_workspace_bytes(tokens, features), B.adatopk_muon_update_workspace_bytes(hidden, features),
+                   B.adatopk_fp8_product_workspace_bytes(tokens, hidden, features), B.adatopk_fp8_product_workspace_bytes(tokens, features, hidden))
+        if need > self.workspace.numel():
+            self.workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+        # what goes into a product and is done with behind it
+        self.narrow, self.wide = B.new_fp8(tokens, features), B.new_fp8(tokens, hidden)
+        self.put_away()
+
+    def put_away(self) -> None:
+        for name, (straight, across) in self.eight.items():
+            B.adatopk_fp8_store_weight(getattr(self, name), straight, across)
+
+    def forward(self, x: torch.Tensor, m: int) -> torch.Tensor:
+        kept, z, out = self.kept[m], torch.empty(self.tokens, self.hidden, dtype=self.dtype, device="cuda"), torch.empty_like(x)
+        B.adatopk_rmsnorm_forward(x, self.weight, EPS, None, kept["rstd"], act8=kept["h"], fp8=self.narrow)  # the weighted rows are wanted in 8 bits alone
+        B.adatopk_fp8_product(self.narrow, self.eight["w1"][0], self.features, z, self.workspace, bias=self.b1)
+        B.adatopk_gelu_forward(z, z, kept["z"], kept["g"], tanh=True)
+        B.adatopk_fp8_store(z, self.wide)
+        B.adatopk_fp8_product(self.wide, self.eight["w2"][0], self.hidden, out, self.workspace, bias=self.b2, add=x)
+        return out
+
+    def backward(self, dout: torch.Tensor, m: int) -> torch.Tensor:
+        kept, g, dz, dx = self.kept[m], self.grad, torch.empty(self.tokens, self.hidden, dtype=self.dtype, device="cuda"), torch.empty_like(dout)
+        B.adatopk_weight_grad(dout, kept["g"], g["w2"], g["b2"], self.workspace, accumulate=True)
+        B.adatopk_fp8_store(dout, self.narrow)
+        B.adatopk_fp8_product(self.narrow, self.eight["w2"][1], self.features, dz, self.workspace)
+        B.adatopk_gelu_backward(dz, kept["z"], dz, tanh=True)
+        B.adatopk_weight_grad(dz, kept["h"], g["w1"], g["b1"], self.workspace, weight=self.weight, accumulate=True)
+        B.adatopk_fp8_store(dz, self.wide)
+        B.adatopk_fp8_product(self.wide, self.eight["w1"][1], self.hidden, dx, self.workspace)
+        B.adatopk_rmsnorm_backward(dx, None, kept["h"], kept["rstd"], self.weight, dx, g["weight"], self.workspace, dsum=dout, accumulate=True)
+        return dx
+
+    def update(self, rate: float = 0.02, decay: float = 0.1, mu: float = 0.95) -> None:
+        """The projections' weights after a step's last micro-batch."""
+        for name in self.eight:
+            B.adatopk_muon_update(self.grad[name], self.momentum[name], mu, True, getattr(self, name), -rate, 1.0 - rate * decay, self.workspace)
+        self.put_away()
+
+
 class Link:
     """One direction of a slow link: a dense tensor as a message of its k largest values, and back."""
 
@@ -96,21 +148,30 @@ def train_step(stage: FeedForwardStage, inputs, gradients, link_in: Link, link_o
     return outs, dxs
 
 
-def main(features: int = 1024, hidden: int = 4096, tokens: int = 2048, micro_batches: int = 4, ratio: float = 4.0) -> None:
-    stage = FeedForwardStage(features, hidden, tokens, micro_batches)
+def main(features: int = 1024, hidden: int = 4096, tokens: int = 2048, micro_batches: int = 4, ratio: float = 4.0, eight_bit: bool = False) -> None:
+    stage = (EightBitStage if eight_bit else FeedForwardStage)(features, hidden, tokens, micro_batches)
     link_in, link_out = Link(tokens * features, ratio), Link(tokens * features, ratio)
     xs = [torch.randn(tokens, features, device="cuda").to(torch.bfloat16) for _ in range(micro_batches)]
     ds = [(torch.randn(tokens, features, device="cuda") * 1e-3).to(torch.bfloat16) for _ in range(micro_batches)]
-    train_step(stage, xs, ds, link_in, link_out)
+
+    def step():
+        train_step(stage, xs, ds, link_in, link_out)
+        if eight_bit:
+            stage.update()
+
+    step()
     begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     begin.record()
-    train_step(stage, xs, ds, link_in, link_out)
+    step()
     end.record()
     torch.cuda.synchronize()
     plain = 2 * tokens * (2 * features + 2 * hidden)  # x, a, z and g in 16 bits
-    print("%d micro-batches of %d tokens, %d -> %d -> %d: %.2f ms a step; %.1f MB kept per micro-batch (%.1f MB in 16 bits); |dW1| = %.3e" % (
-        micro_batches, tokens, features, hidden, features, begin.elapsed_time(end), stage.kept_bytes() / 1e6, plain / 1e6, float(stage.grad["w1"].norm())))
+    print("%d micro-batches of %d tokens, %d -> %d -> %d%s: %.2f ms a step; %.1f MB kept per micro-batch (%.1f MB in 16 bits); |dW1| = %.3e" % (
+        micro_batches, tokens, features, hidden, features, " in 8 bits" if eight_bit else "", begin.elapsed_time(end), stage.kept_bytes() / 1e6, plain / 1e6,
+        float(stage.grad["w1"].norm())))
 
 
 if __name__ == "__main__":
-    main()
+    parser = argparse.ArgumentParser(description="A pipeline stage's training step between two compressed links.")
+    parser.add_argument("--eight-bit", action="store_true", help="projections in 8-bit floating point, their weights updated")
+    main(eight_bit=parser.parse_args().eight_bit)
