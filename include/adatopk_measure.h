@@ -67,6 +67,7 @@ size_t adatopk_measure_workspace_offset(int32_t what, int64_t n_total, int32_t n
  *                                shares of the rows in which it is, apart from them
  *   fp8_product  out[0]          side of a tile, 0: a few tokens     out[1]  1: the tile's wavefronts take turns along the sum
  *                out[2]          shares of the sum; more than one are joined by a second kernel
+ *                out[3]          1: the tiles behind the last full round are done in quarters
  *   muon_update  eight products, three numbers each (sides of a tile, and what out[2] is above, + 64 where its wavefronts take turns along the sum): X X^T, A A,
  *                B X and the last step's B X, which writes w, from pairs, then from their h alone */
 adatopk_status adatopk_measure_weight_grad_cut(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, int64_t dy_stride, int32_t *out);

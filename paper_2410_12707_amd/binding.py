@@ -894,10 +894,10 @@ def measure_layernorm_cut(rows: int, cols: int, backward: bool):
 
 
 def measure_fp8_product_cut(rows: int, n_out: int, n_in: int, dtype: torch.dtype):
-    """(side of a tile or 0 for a few tokens, whether its wavefronts take turns along the sum, shares of the sum) of a product."""
-    out = (ctypes.c_int32 * 3)()
+    """(side of a tile or 0 for a few tokens, whether its wavefronts take turns along the sum, shares of the sum, whether the last tiles are in quarters) of a product."""
+    out = (ctypes.c_int32 * 4)()
     _check(load_measure_library().adatopk_measure_fp8_product_cut(int(rows), int(n_out), int(n_in), _dtype_code(dtype), out), "adatopk_measure_fp8_product_cut")
-    return out[0], bool(out[1]), out[2]
+    return out[0], bool(out[1]), out[2], bool(out[3])
 
 
 def measure_muon_update_cut(rows: int, cols: int):

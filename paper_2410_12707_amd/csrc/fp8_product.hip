@@ -60,16 +60,14 @@ struct Source {
     __device__ __forceinline__ uint64_t scales_b(int t) const { return sb + static_cast<uint64_t>(t) * scale_pitch_b; }
 };
 
-template <typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Tile::NT, PER_CU * Tile::NT / 256) void k_fp8_product(Product f) {
-    constexpr int MI = Tile::MI, NI = Tile::NI;
-    constexpr int PITCH = MI * 32 + 4;  // floats from one token's results to the next in LDS
-    constexpr int RESULTS = Tile::WAVES * 32 * PITCH * 4;
+// Bytes of LDS: the tile's buffers, and behind the sums its results.
+template <typename Tile> constexpr int RESULTS_PITCH = Tile::MI * 32 + 4;  // floats from one token's results to the next
+template <typename Tile> constexpr int LDS_BYTES = Tile::LDS > Tile::WAVES * 32 * RESULTS_PITCH<Tile> * 4 ? Tile::LDS : Tile::WAVES * 32 * RESULTS_PITCH<Tile> * 4;
+
+// The tile from feature out0 and token row0 on, of share `part` of the sum.
+template <typename T, typename Tile> __device__ __forceinline__ void product_of_tile(const Product &f, char *lds, int64_t out0, int64_t row0, int part) {
+    constexpr int MI = Tile::MI, NI = Tile::NI, PITCH = RESULTS_PITCH<Tile>;
     static_assert(Tile::ALONG == 1 || Tile::BN * PITCH * 4 <= Tile::GROUP_LDS, "a group's results fit its buffers");
-    __shared__ __attribute__((aligned(16))) char lds[Tile::LDS > RESULTS ? Tile::LDS : RESULTS];
-    const int tiles = f.tiles_out * f.tiles_rows, b = place(blockIdx.x, gridDim.x), part = b / tiles;
-    int tile_out, tile_row;
-    tile_at(b - part * tiles, f.tiles_out, f.tiles_rows, tile_out, tile_row);
-    const int64_t out0 = static_cast<int64_t>(tile_out) * Tile::BM, row0 = static_cast<int64_t>(tile_row) * Tile::BN;
     const int first = part * f.slices_per_split, slices = f.slices - first < f.slices_per_split ? f.slices - first : f.slices_per_split;
     const Source source{reinterpret_cast<uint64_t>(f.w.q + out0 * f.w.pitch + first * static_cast<int64_t>(SLICE)),
                         reinterpret_cast<uint64_t>(f.x.q + row0 * f.x.pitch + first * static_cast<int64_t>(SLICE)),
@@ -165,6 +163,31 @@ template <typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Ti
     }
 }
 
+template <typename T, typename Tile, int PER_CU> __global__ __launch_bounds__(Tile::NT, PER_CU * Tile::NT / 256) void k_fp8_product(Product f) {
+    __shared__ __attribute__((aligned(16))) char lds[LDS_BYTES<Tile>];
+    const int tiles = f.tiles_out * f.tiles_rows, b = place(blockIdx.x, gridDim.x), part = b / tiles;
+    int tile_out, tile_row;
+    tile_at(b - part * tiles, f.tiles_out, f.tiles_rows, tile_out, tile_row);
+    product_of_tile<T, Tile>(f, lds, static_cast<int64_t>(tile_out) * Tile::BM, static_cast<int64_t>(tile_row) * Tile::BN, part);
+}
+
+// The same with the first `whole` tiles as they are and each of the others in four, so that what is left behind the last full round of the chip is done in a
+// part of a round's time.
+template <typename T, typename Tile, typename Quarter> __global__ __launch_bounds__(Tile::NT, Tile::NT / 256) void k_fp8_product_quartered(Product f, int whole) {
+    static_assert(Quarter::NT == Tile::NT && 2 * Quarter::BM == Tile::BM && 2 * Quarter::BN == Tile::BN && LDS_BYTES<Quarter> <= LDS_BYTES<Tile>, "a quarter");
+    __shared__ __attribute__((aligned(16))) char lds[LDS_BYTES<Tile>];
+    const int b = blockIdx.x;
+    const bool all = b < whole;
+    const int at = all ? place(b, whole) : place(b - whole, gridDim.x - whole);
+    int tile_out, tile_row;
+    tile_at(all ? at : whole + at / 4, f.tiles_out, f.tiles_rows, tile_out, tile_row);
+    int64_t out0 = static_cast<int64_t>(tile_out) * Tile::BM, row0 = static_cast<int64_t>(tile_row) * Tile::BN;
+    if (all) return product_of_tile<T, Tile>(f, lds, out0, row0, 0);
+    out0 += at % 2 * Quarter::BM;
+    row0 += at % 4 / 2 * Quarter::BN;
+    if (out0 < f.n_out && row0 < f.rows) product_of_tile<T, Quarter>(f, lds, out0, row0, 0);
+}
+
 // Partial sums added up in the order of the sum's axis.  An octet of a row per thread.
 template <typename T> __global__ __launch_bounds__(256) void k_fp8_join(Product f, Divisor per_row, uint32_t octets) {
     const uint32_t t = blockIdx.x * 256u + threadIdx.x;
@@ -254,6 +277,7 @@ template <typename T, int TJ> __global__ __launch_bounds__(FEW_WAVES * 64) void 
 enum Form { LARGE, MIDDLE, SMALL, DEEP, TILED, FEW = TILED, NONE };
 template <Kind KIND> struct Tiles {
     using Large = RowTile<KIND, 256, 256, 2, 4, 2>;
+    using Quarter = RowTile<KIND, 128, 128, 2, 4, 2>;  // of Large, by as many wavefronts
     using Middle = RowTile<KIND, 128, 128, 2, 2, 2>;
     using Small = RowTile<KIND, 64, 64, 2, 2, 2>;
     using Deep = RowTile<KIND, 64, 64, 1, 1, 2, 4>;
@@ -263,19 +287,24 @@ constexpr int SIDE[TILED] = {256, 128, 64, 64}, SLOTS[TILED] = {256, 512, 1024, 
 struct Cut {
     Form form;
     int tiles_out, tiles_rows, slices, split, per;
+    int whole;  // tiles; the others in quarters
 };
 // us: of a slice of 128 for a workgroup with a few others on the chip and on a full one, and what a workgroup takes beside; by the 8-bit instruction, and as bf16 for fp32
 // results.  Measured at 14 sizes, 65 x 768 x 768 to 16384 x 1600 x 6400: by tile 193, 216, 302, 550 us there, 57, 69, 115, 140 for 4096 x 4096 x 4096, 17, 8.6, 6.0, 6.4
 // for 1024 x 1024 x 1024, 57, 24, 17, 11 for 128 x 6400 x 1600.
 constexpr double STEP_ALONE[2][TILED] = {{1.0, 0.38, 0.25, 0.125}, {1.95, 0.66, 0.38, 0.2}}, STEP_FULL[2][TILED] = {{1.5, 0.88, 0.69, 0.16}, {3.1, 1.7, 1.1, 0.26}};
 constexpr double BESIDE[2][TILED] = {{8., 6., 4.8, 5.}, {10., 8., 5.5, 5.3}};
+// Up to so many of the largest tiles behind the last full round are done in quarters, all at a time.  16384 x 6400 by 512, 1600, 4096 (64 of them): 109, 191, 364 us
+// without, 99, 185, 353 with; of 160 and 224, where the quarters go round, 53 without and 58 with, 54 and 63 (8192 x 3328 and 3840 by 1600).
+constexpr int64_t QUARTERED = 64;
+constexpr double QUARTER_STEP[2] = {0.5, 0.9}, QUARTER_BESIDE[2] = {6., 8.};
 // Up to so many tokens k_fp8_few is as quick or quicker: 16 tokens, 1600 x 6400, 5.3 us against 6.6, 32 tokens, 6400 x 1600, 10.9 against 12.2; 48, 1600 x 6400, 10.5
 // against 7.0.
 constexpr int64_t FEW_ROWS = 32;
 constexpr int SPLIT_MAX = 16;
 Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in, bool exact) {
     const int slices = static_cast<int>(adatopk_internal::fp8_pitch(n_in) / SLICE);
-    Cut best{FEW, 0, 0, slices, 1, slices};
+    Cut best{FEW, 0, 0, slices, 1, slices, 0};
     if (slices == 0) best.form = NONE;  // (nothing to add up: what the join adds to no shares)
     if (rows <= FEW_ROWS || slices == 0) return best;
     double least = 0;
@@ -289,10 +318,16 @@ Cut cut_of(int64_t rows, int64_t n_out, int64_t n_in, bool exact) {
             const double rounds = filled <= 1. ? 1. : SLOTS[t] > 256 ? filled : static_cast<double>((tiles * split + 255) / 256);
             const double step = STEP_ALONE[exact][t] + some * (STEP_FULL[exact][t] - STEP_ALONE[exact][t]);
             const double join = split == 1 ? 0. : 4.5 + 0.4e-6 * 4. * split * static_cast<double>(rows) * static_cast<double>(n_out);
-            const double cost = rounds * (BESIDE[exact][t] + step * per) + join;
+            const double one = BESIDE[exact][t] + step * per;
+            double cost = rounds * one + join;
+            int64_t left = 0;  // tiles in quarters
+            if (t == LARGE && split == 1 && tiles > 256 && tiles % 256 != 0 && tiles % 256 <= QUARTERED) {
+                left = tiles % 256;
+                cost -= one - QUARTER_BESIDE[exact] - QUARTER_STEP[exact] * per;
+            }
             if (best.form == FEW || cost < least) {
                 least = cost;
-                best = Cut{static_cast<Form>(t), static_cast<int>(out), static_cast<int>(along), slices, split, per};
+                best = Cut{static_cast<Form>(t), static_cast<int>(out), static_cast<int>(along), slices, split, per, static_cast<int>(tiles - left)};
             }
         }
     }
@@ -350,7 +385,10 @@ adatopk_status adatopk_fp8_product(const void *fp8_x, const void *fp8_w, int64_t
         }
         using Of = Tiles<sizeof(T) == 4 ? FP8_EXACT : FP8_FAST>;
         const dim3 groups(static_cast<unsigned>(c.tiles_out * c.tiles_rows * c.split));
-        if (c.form == LARGE)
+        if (c.form == LARGE && c.whole < c.tiles_out * c.tiles_rows)
+            hipLaunchKernelGGL((k_fp8_product_quartered<T, typename Of::Large, typename Of::Quarter>), dim3(static_cast<unsigned>(c.whole + 4 * (c.tiles_out * c.tiles_rows - c.whole))),
+                               dim3(Of::Large::NT), 0, st, f, c.whole);
+        else if (c.form == LARGE)
             hipLaunchKernelGGL((k_fp8_product<T, typename Of::Large, 1>), groups, dim3(Of::Large::NT), 0, st, f);
         else if (c.form == MIDDLE)
             hipLaunchKernelGGL((k_fp8_product<T, typename Of::Middle, 2>), groups, dim3(Of::Middle::NT), 0, st, f);
@@ -370,6 +408,7 @@ adatopk_status adatopk_measure_fp8_product_cut(int64_t rows, int64_t n_out, int6
     out[0] = c.form == FEW ? 0 : SIDE[c.form];
     out[1] = c.form == DEEP ? 1 : 0;
     out[2] = c.split;
+    out[3] = c.form == LARGE && c.whole < c.tiles_out * c.tiles_rows ? 1 : 0;
     return ADATOPK_OK;
 }
 #endif

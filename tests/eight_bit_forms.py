@@ -3,17 +3,17 @@ import torch
 
 BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
 
-# type, (side of a tile or 0 for a few tokens, wavefronts along the sum, sum shared out), (rows, n_out, n_in): odd sizes, tiles that end outside the matrix
+# type, (side of a tile or 0 for a few tokens, wavefronts along the sum, sum shared out, last tiles in quarters), (rows, n_out, n_in): odd sizes, tiles that end outside the matrix
 PRODUCTS = [
-    (BF16, (0, False, False), (7, 33, 391)), (BF16, (0, False, False), (31, 257, 1155)),
-    (BF16, (64, True, False), (45, 77, 903)), (BF16, (64, True, True), (35, 70, 5256)),
-    (BF16, (64, False, False), (1027, 2051, 515)), (BF16, (64, False, True), (4210, 7, 11138)),
-    (BF16, (128, False, False), (1500, 5003, 389)), (BF16, (128, False, True), (11242, 77, 7172)),
-    (BF16, (256, False, False), (3001, 4099, 900)), (BF16, (256, False, True), (134, 5741, 58402)),
-    (F32, (0, False, False), (7, 33, 391)), (F32, (64, True, False), (45, 77, 903)), (F32, (64, True, True), (35, 70, 5256)),
-    (F32, (64, False, False), (1027, 2051, 515)), (F32, (64, False, True), (16946, 5, 2491)),
-    (F32, (128, False, False), (1500, 5003, 389)), (F32, (128, False, True), (11113, 81, 10687)),
-    (F32, (256, False, False), (3001, 4099, 900)), (F32, (256, False, True), (10475, 491, 15257)),
+    (BF16, (0, False, False, False), (7, 33, 391)), (BF16, (0, False, False, False), (31, 257, 1155)),
+    (BF16, (64, True, False, False), (45, 77, 903)), (BF16, (64, True, True, False), (35, 70, 5256)),
+    (BF16, (64, False, False, False), (1027, 2051, 515)), (BF16, (64, False, True, False), (4210, 7, 11138)),
+    (BF16, (128, False, False, False), (1500, 5003, 389)), (BF16, (128, False, True, False), (11242, 77, 7172)),
+    (BF16, (256, False, False, False), (3001, 4099, 900)), (BF16, (256, False, False, True), (16100, 6300, 390)), (BF16, (256, False, True, False), (134, 5741, 58402)),
+    (F32, (0, False, False, False), (7, 33, 391)), (F32, (64, True, False, False), (45, 77, 903)), (F32, (64, True, True, False), (35, 70, 5256)),
+    (F32, (64, False, False, False), (1027, 2051, 515)), (F32, (64, False, True, False), (16946, 5, 2491)),
+    (F32, (128, False, False, False), (1500, 5003, 389)), (F32, (128, False, True, False), (11113, 81, 10687)),
+    (F32, (256, False, False, False), (3001, 4099, 900)), (F32, (256, False, False, True), (16100, 6300, 390)), (F32, (256, False, True, False), (10475, 491, 15257)),
 ]
 
 # which of an update's eight products, its tile, wavefronts along the sum, sum shared out, (rows, cols)

@@ -143,8 +143,8 @@ def test_the_binding_refuses(monkeypatch):
 
 def test_sizes_for_every_form_take_the_form_they_are_meant_for():
     for dtype, form, size in forms.PRODUCTS:
-        side, along, split = B.measure_fp8_product_cut(*size, dtype)
-        assert (side, along, split > 1) == form, (dtype, size, side, along, split)
+        side, along, split, quarters = B.measure_fp8_product_cut(*size, dtype)
+        assert (side, along, split > 1, quarters) == form, (dtype, size, side, along, split, quarters)
     for which, tile, along, shared, size in forms.UPDATES:
         cut = B.measure_muon_update_cut(*size)[which]
         assert (cut[0], cut[1], cut[2] > 1) == (tile, along, shared), (which, size, cut)
@@ -162,8 +162,8 @@ def test_there_is_no_other_form():
     for _ in range(10000):
         for dtype, table in known.items():
             rows, n_out, n_in = size(70000), size(131072), size(131072)
-            side, along, split = B.measure_fp8_product_cut(rows, n_out, n_in, dtype)
-            assert (side, along, split > 1) in table, (rows, n_out, n_in, dtype)
+            side, along, split, quarters = B.measure_fp8_product_cut(rows, n_out, n_in, dtype)
+            assert (side, along, split > 1, quarters) in table, (rows, n_out, n_in, dtype)
             assert split == 1 or B.adatopk_fp8_product_workspace_bytes(rows, n_out, n_in) >= split * rows * n_out * 4
     table = {(which, tile, along, shared) for which, tile, along, shared, _ in forms.UPDATES}
     for _ in range(10000):

@@ -317,3 +317,88 @@ def test_scales_from_end_to_end(dtype, rows):
     expected = x @ w.T
     expected[:, 3] = np.inf
     assert np.array_equal(ref.host(y), expected)
+
+
+def test_a_weight_that_is_only_written():
+    # decay 0: what w held is not looked at, nor is a gradient's or a weight's neighbourhood written
+    g, ws = torch.randn(70, 90, device="cuda"), torch.empty(B.adatopk_muon_update_workspace_bytes(70, 90), dtype=torch.uint8, device="cuda")
+    w, plain = torch.full((70, 90), float("nan"), device="cuda"), torch.zeros(70, 90, device="cuda")
+    for out in (w, plain):
+        B.adatopk_muon_update(g, None, 0.0, False, out, 1.0, 0.0, ws)
+    assert torch.equal(w, plain)
+    kept = g.clone()
+    B.adatopk_muon_update(g, None, 0.0, False, w, 0.0, 1.0, ws)  # and one that is left as it is
+    assert torch.equal(w, plain) and torch.equal(g, kept)
+
+
+def test_matrices_past_32_bits():
+    rows, cols, some = 140000, 32768, 300
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(rows, cols, dtype=BF16, device="cuda")
+    for top in range(0, rows, 20000):
+        x[top:top + 20000].copy_(torch.randn(20000, cols, device="cuda", generator=gen))
+    buffer, back, y = B.new_fp8(rows, cols), torch.empty_like(x), torch.empty_like(x)
+    last, few = x[-some:].clone(), B.new_fp8(some, cols)
+    want = torch.empty_like(last)
+    B.adatopk_fp8_store(x, buffer)
+    B.adatopk_fp8_load(buffer, back)
+    B.adatopk_fp8_store(last, few)
+    B.adatopk_fp8_load(few, want)
+    assert torch.equal(back[-some:], want)
+    # its products with a few features, whose sums may be cut into other shares
+    w = torch.randn(40, cols, device="cuda", generator=gen) * cols ** -0.5
+    w8, held = B.new_fp8(40, cols), torch.empty(40, cols, device="cuda")
+    B.adatopk_fp8_store_weight(w, w8)
+    B.adatopk_fp8_load(w8, held)
+    z = torch.empty(rows, 40, device="cuda")
+    B.adatopk_fp8_product(buffer, w8, cols, z, torch.empty(max(B.adatopk_fp8_product_workspace_bytes(rows, 40, cols), 256), dtype=torch.uint8, device="cuda"))
+    a, b = want.double(), held.double()
+    bound = (a.abs() @ b.abs().t().contiguous()) * (2 * ref.U * (8 + 2 * cols ** 0.5))
+    assert bool(((z[-some:].double() - a @ b.t().contiguous()).abs() <= bound).all())
+    # the norm, its backward pass, and what it puts away
+    rstd, act8 = torch.empty(rows, device="cuda"), B.new_act8(rows, cols)
+    B.adatopk_rmsnorm_forward(x, None, 1e-5, y, rstd, act8=act8, fp8=buffer)
+    B.adatopk_fp8_load(buffer, back)
+    few_rstd, few_act8 = torch.empty(some, device="cuda"), B.new_act8(some, cols)
+    B.adatopk_rmsnorm_forward(last, None, 1e-5, want, few_rstd, act8=few_act8, fp8=few)
+    assert torch.equal(y[-some:], want) and torch.equal(rstd[-some:], few_rstd)
+    B.adatopk_fp8_load(few, want)
+    assert torch.equal(back[-some:], want)
+    B.adatopk_rmsnorm_backward(x, None, act8, rstd, None, y, None, None)
+    B.adatopk_rmsnorm_backward(last, None, few_act8, few_rstd, None, want, None, None)
+    assert torch.equal(y[-some:], want)
+
+
+def test_weights_past_32_bits():
+    rows, cols, some = 70100, 65000, 200
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.empty(rows, cols, dtype=BF16, device="cuda")
+    for top in range(0, rows, 10000):
+        w[top:top + 10000].copy_(torch.randn(min(10000, rows - top), cols, device="cuda", generator=gen))
+    first = rows // 128 * 128 - 128  # where a tile begins
+    part = w[first:].clone()
+    straight, across, few = B.new_fp8(rows, cols), B.new_fp8(cols, rows), B.new_fp8(*part.shape)
+    B.adatopk_fp8_store_weight(w, straight, across)
+    B.adatopk_fp8_store_weight(part, few)
+    back, want = torch.empty_like(w), torch.empty_like(part)
+    B.adatopk_fp8_load(few, want)
+    B.adatopk_fp8_load(straight, back)
+    assert torch.equal(back[first:], want)
+    turned = back.view(cols, rows)
+    B.adatopk_fp8_load(across, turned)
+    assert torch.equal(turned[-some:, first:], want[:, -some:].t())
+
+
+def test_an_update_past_32_bits():
+    # a gradient of rank one, u v': its one singular value is the polynomial's value at 1, all else of X stays nothing
+    rows, cols = 33000, 64001
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    u, v = torch.randn(rows, 1, device="cuda", generator=gen), torch.randn(1, cols, device="cuda", generator=gen)
+    w, ws = torch.empty(rows, cols, device="cuda"), torch.empty(B.adatopk_muon_update_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    B.adatopk_muon_update(u @ v, None, 0.0, False, w, 1.0, 0.0, ws, steps=1)
+    factor = (3.4445 - 4.7750 + 2.0315) / (float(u.double().norm()) * float(v.double().norm()))
+    # a x, b x^3 and c x^5 are off by some roundings of 2^-22 each: of 10.3 that cancel to 0.7, and of the elements' pairs, of which the smallest lose bits to
+    # fp16's subnormals: 2^-25 of 2^14, the size of X's norm
+    for rows_of in (slice(0, 500), slice(rows - 500, rows)):
+        want = u[rows_of].double() @ v.double() * factor
+        assert float((w[rows_of].double() - want).norm() / want.norm()) <= 4 * 10.3 / 0.701 * 2.0 ** -22 + float(2.0 ** -39 * (500 * cols) ** 0.5 / want.norm())
