@@ -33,15 +33,20 @@ using namespace adatopk_stage;
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float ONE = 16384.f, ONE_OF_B = 8192.f;  // what 1 is held as
 
-// A matrix of pairs: rows of 128 bytes for 32 elements, 32 h and then their l, padded with zeros.
+// A matrix of pairs: rows of 2^run h and then their l, and so on, padded with zeros.  Runs of 32 where products take both (128 bytes are 32 elements), of 64 where
+// they take the h alone (128 bytes are 64, and the other half of no line is fetched with them).
 struct Pairs {
     uint8_t *at;
     int64_t pitch;
+    int run;
 };
+constexpr int run_for(bool high) { return high ? 6 : 5; }
 constexpr int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
 inline size_t pairs_bytes(int64_t rows, int64_t cols) { return adatopk_internal::align_up(static_cast<size_t>(rows) * static_cast<size_t>(padded(cols)) * 4, 256); }
 
-__device__ __forceinline__ uint8_t *octet_of(const Pairs &p, int64_t row, int64_t col) { return p.at + row * p.pitch + col / 32 * 128 + col % 32 * 2; }
+__device__ __forceinline__ uint8_t *octet_of(const Pairs &p, int64_t row, int64_t col) {
+    return p.at + row * p.pitch + ((col >> p.run) << (p.run + 2)) + (col & ((1 << p.run) - 1)) * 2;
+}
 // Eight elements of a row from col on, a multiple of eight; those from `limit` on are zeros, and what lies behind its padding is left alone.
 __device__ __forceinline__ void put_pairs(const Pairs &p, int64_t row, int64_t col, int64_t limit, const float (&v)[8]) {
     if (col >= padded(limit)) return;
@@ -54,13 +59,13 @@ __device__ __forceinline__ void put_pairs(const Pairs &p, int64_t row, int64_t c
     }
     uint8_t *const to = octet_of(p, row, col);
     *reinterpret_cast<U4 *>(to) = pack<F16>(h).w[0];
-    *reinterpret_cast<U4 *>(to + 64) = pack<F16>(l).w[0];
+    *reinterpret_cast<U4 *>(to + (2 << p.run)) = pack<F16>(l).w[0];
 }
 __device__ __forceinline__ void get_pairs(const Pairs &p, int64_t row, int64_t col, float (&v)[8]) {
     const uint8_t *const from = octet_of(p, row, col);
     float l[8];
     unpack(Raw<F16>{{*reinterpret_cast<const U4 *>(from)}}, v);
-    unpack(Raw<F16>{{*reinterpret_cast<const U4 *>(from + 64)}}, l);
+    unpack(Raw<F16>{{*reinterpret_cast<const U4 *>(from + (2 << p.run))}}, l);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += l[j];
 }
@@ -410,15 +415,17 @@ constexpr int SPLIT_MAX = 16;
 // from pairs (with the join) 80, -, -, 68, 82, from the h alone 51, -, -, 48, 87; A A 45, -, -, 35, 30 and 34, -, -, 34, 24.
 constexpr double STEP[2][SHAPES] = {{2.3, 2.05, 1.85, 1.45, 0.72}, {2.0, 1.95, 2.1, 1.5, 1.1}}, BESIDE[SHAPES] = {14., 12., 11., 8., 5.};
 constexpr double DEEP_STEP = 0.17;  // of Deep64
-Choice choice_of(int64_t rows_a, int64_t rows_b, int64_t sum, bool symmetric, bool may_turn, bool high) {
+enum Writes { HALF, X, X_AS_IT_LIES, W };  // a symmetric matrix; X, either operand first or the first one; w
+Choice choice_of(int64_t rows_a, int64_t rows_b, int64_t sum, Writes writes, bool high) {
+    const bool symmetric = writes == HALF, x = writes == X || writes == X_AS_IT_LIES;
     Choice best{SHAPES, high, false, 1, 0};
     double least = 0;
     const int slices = static_cast<int>(padded(sum) / (high ? 64 : 32));
     for (int t = 0; t < SHAPES; ++t)
-        for (int turned = 0; turned < (may_turn && SHAPE_BM[t] != SHAPE_BN[t] ? 2 : 1); ++turned) {
+        for (int turned = 0; turned < (writes == X && SHAPE_BM[t] != SHAPE_BN[t] ? 2 : 1); ++turned) {
             if (symmetric && SHAPE_BM[t] != SHAPE_BN[t]) continue;
             // X's tiles have to reach to the end of its last 64, whose zeros they write
-            if (may_turn && padded(turned ? rows_b : rows_a) > ((turned ? rows_b : rows_a) + SHAPE_BM[t] - 1) / SHAPE_BM[t] * SHAPE_BM[t]) continue;
+            if (x && padded(turned ? rows_b : rows_a) > ((turned ? rows_b : rows_a) + SHAPE_BM[t] - 1) / SHAPE_BM[t] * SHAPE_BM[t]) continue;
             const int64_t a = ((turned ? rows_b : rows_a) + SHAPE_BM[t] - 1) / SHAPE_BM[t], b = ((turned ? rows_a : rows_b) + SHAPE_BN[t] - 1) / SHAPE_BN[t];
             for (int split = 1; split <= (symmetric ? SPLIT_MAX : 1) && split <= slices; ++split) {
                 const int per = (slices + split - 1) / split;
@@ -516,8 +523,8 @@ Workspace workspace_of(int64_t less, int64_t more) {
     w.squares = take(MIX_GROUPS * sizeof(double));
     size_t most = 0;
     for (int high = 0; high < 2; ++high) {
-        w.gram_of[high] = choice_of(less, less, more, true, false, high != 0);
-        w.poly_of[high] = choice_of(less, less, less, true, false, high != 0);
+        w.gram_of[high] = choice_of(less, less, more, HALF, high != 0);
+        w.poly_of[high] = choice_of(less, less, less, HALF, high != 0);
         for (const Choice &c : {w.gram_of[high], w.poly_of[high]})
             if (const size_t bytes = shares_bytes(c, less); bytes > most) most = bytes;
     }
@@ -547,8 +554,12 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
     const Workspace at = workspace_of(less, more);
     if (workspace_bytes < at.bytes) return ADATOPK_EWORKSPACE;
     uint8_t *const base = static_cast<uint8_t *>(workspace);
-    const auto pairs = [&](size_t where, int64_t of) { return Pairs{base + where, padded(of) * 4}; };
-    const Pairs x = pairs(at.x, more), gram = pairs(at.gram, less), poly = pairs(at.poly, less);
+    // Where w is of 16 bits: products of 11 bits in all steps but the last ones, and in bf16's last.
+    const bool coarser = dt != ADATOPK_F32 && less >= COARSE_FROM, coarse_end = coarser && dt == ADATOPK_BF16;
+    const int fine = !coarser ? steps : dt == ADATOPK_F16 ? 3 : 2;
+    const auto high_at = [&](int step) { return steps - step > fine || (coarse_end && step + 1 == steps); };
+    const auto pairs = [&](size_t where, int64_t of) { return Pairs{base + where, padded(of) * 4, run_for(high_at(0))}; };
+    Pairs x = pairs(at.x, more), gram = pairs(at.gram, less), poly = pairs(at.poly, less);
     Pairs xt = pairs(at.xt[0], less), xt_next = pairs(at.xt[1], less);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
 
@@ -564,13 +575,13 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
     });
 
     const int along = static_cast<int>(padded(more) / 32), side = static_cast<int>(padded(less) / 32);
-    // Where w is of 16 bits: products of 11 bits in all steps but the last ones, and in bf16's last.
-    const bool coarser = dt != ADATOPK_F32 && less >= COARSE_FROM, coarse_end = coarser && dt == ADATOPK_BF16;
-    const int fine = !coarser ? steps : dt == ADATOPK_F16 ? 3 : 2;
-    const Choice next = choice_of(less, more, less, false, true, false), next_coarse = choice_of(less, more, less, false, true, true);
-    const Choice last = choice_of(cols, rows, less, false, false, coarse_end);
+    const Choice next = choice_of(less, more, less, X, false), next_coarse = choice_of(less, more, less, X, true);
+    // (X's runs change: turned, it would be read and written in place in two orders)
+    const Choice next_changing = choice_of(less, more, less, X_AS_IT_LIES, true);
+    const Choice last = choice_of(cols, rows, less, W, coarse_end);
     for (int step = 0; step < steps; ++step) {
-        const bool high = steps - step > fine || (coarse_end && step + 1 == steps);
+        const bool high = high_at(step);
+        x.run = xt.run = gram.run = poly.run = run_for(high);
         Product p{};
         p.partial = reinterpret_cast<float *>(base + at.shares);
         p.a = p.b = x;
@@ -590,10 +601,11 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
             p.rows_b = more;
             p.by_j = xt_next;
             p.by_i = x;
+            p.by_j.run = p.by_i.run = run_for(high_at(step + 1));
             p.old_by_j = xt;
             p.old_by_i = x;
             if (coarse)
-                launch_product<NEXT, float, HIGH>(p, next_coarse, st);
+                launch_product<NEXT, float, HIGH>(p, high_at(step + 1) ? next_coarse : next_changing, st);
             else
                 launch_product<NEXT, float, PAIRS>(p, next, st);
             const Pairs t = xt;
@@ -625,8 +637,8 @@ adatopk_status adatopk_measure_muon_update_cut(int64_t rows, int64_t cols, int32
     if (!update_ok(rows, cols) || rows == 0 || cols == 0) return ADATOPK_EINVAL;
     const int64_t less = rows < cols ? rows : cols, more = rows < cols ? cols : rows;
     for (int high = 0; high < 2; ++high) {
-        const Choice four[] = {choice_of(less, less, more, true, false, high != 0), choice_of(less, less, less, true, false, high != 0),
-                               choice_of(less, more, less, false, true, high != 0), choice_of(cols, rows, less, false, false, high != 0)};
+        const Choice four[] = {choice_of(less, less, more, HALF, high != 0), choice_of(less, less, less, HALF, high != 0),
+                               choice_of(less, more, less, X, high != 0), choice_of(cols, rows, less, W, high != 0)};
         for (int k = 0; k < 4; ++k) {
             const Choice &c = four[k];
             const int64_t ra = k < 2 ? less : k == 3 ? cols : c.turned ? more : less, rb = k < 2 ? less : k == 3 ? rows : c.turned ? less : more;

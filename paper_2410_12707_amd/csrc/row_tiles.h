@@ -96,17 +96,16 @@ template <Kind KIND, int BM_, int BN_, int WM_, int WN_, int STAGES_, int ALONG_
         const int turn = ALONG == 1 ? 0 : place / WAVES;  // slices turn, turn + ALONG, ...
         const int slices = ALONG == 1 ? all_slices : (all_slices - turn + ALONG - 1) / ALONG;
         uint32_t from_a[PA], from_b[PB];
-        const auto piece = [](int c) { return static_cast<uint32_t>(KIND == HIGH ? c / 4 * SLICE + c % 4 * 16 : c * 16); };
         const auto chunk = [&](int eight) { return (lane % 8) ^ (4 * (eight % 2) + lane / 16); };  // of the rows 8 * eight + lane / 8
 #pragma unroll
         for (int q = 0; q < PA; ++q) {
             const int r = (wave * PA + q) * 8 + lane / 8, last = static_cast<int>(source.left_a) - 1;
-            from_a[q] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(source.pitch_a) + piece(chunk(wave * PA + q));
+            from_a[q] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(source.pitch_a) + chunk(wave * PA + q) * 16;
         }
 #pragma unroll
         for (int q = 0; q < PB; ++q) {
             const int r = (wave * PB + q) * 8 + lane / 8, last = static_cast<int>(source.left_b) - 1;
-            from_b[q] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(source.pitch_b) + piece(chunk(wave * PB + q));
+            from_b[q] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(source.pitch_b) + chunk(wave * PB + q) * 16;
         }
         const uint32_t lds0 = lds_address(lds) + turn * GROUP_LDS;
         constexpr int LEAST = BM < BN ? BM : BN;
