@@ -61,11 +61,14 @@ __device__ __forceinline__ void put_pairs(const Pairs &p, int64_t row, int64_t c
     *reinterpret_cast<U4 *>(to) = pack<F16>(h).w[0];
     *reinterpret_cast<U4 *>(to + (2 << p.run)) = pack<F16>(l).w[0];
 }
-__device__ __forceinline__ void get_pairs(const Pairs &p, int64_t row, int64_t col, float (&v)[8]) {
+__device__ __forceinline__ Raw<float> fetch_pairs(const Pairs &p, int64_t row, int64_t col) {
     const uint8_t *const from = octet_of(p, row, col);
+    return Raw<float>{{*reinterpret_cast<const U4 *>(from), *reinterpret_cast<const U4 *>(from + (2 << p.run))}};
+}
+__device__ __forceinline__ void unpack_pairs(const Raw<float> &pairs, float (&v)[8]) {
     float l[8];
-    unpack(Raw<F16>{{*reinterpret_cast<const U4 *>(from)}}, v);
-    unpack(Raw<F16>{{*reinterpret_cast<const U4 *>(from + (2 << p.run))}}, l);
+    unpack(Raw<F16>{{pairs.w[0]}}, v);
+    unpack(Raw<F16>{{pairs.w[1]}}, l);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += l[j];
 }
@@ -189,7 +192,7 @@ __device__ __forceinline__ void tile_below(int tile, int &a, int &b) {
 // B's elements from A's and A A's, both as they are held: i and the seven behind it of row j.
 __device__ __forceinline__ void polynomial(const Product &f, int64_t j, int64_t i, float (&v)[8]) {
     float gram[8] = {};
-    if (j < f.rows_b && i < padded(f.rows_a)) get_pairs(f.gram, j, i, gram);
+    if (j < f.rows_b && i < padded(f.rows_a)) unpack_pairs(fetch_pairs(f.gram, j, i), gram);
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
         v[x] = __builtin_fmaf(v[x], NS_C * (ONE_OF_B / ONE / ONE), gram[x] * (NS_B * (ONE_OF_B / ONE)));
@@ -221,14 +224,25 @@ template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_
     Tile::run(lds, source, slices, acc);
     __syncthreads();  // the buffers have been read
 
+    // What eight results are added to: X as it was, or w.
+    constexpr bool TO_X = MODE == NEXT && Tile::FORM == HIGH, TO_W = MODE == LAST;
+    const auto before = [&](int64_t j, int64_t i) {
+        if constexpr (TO_W) {
+            return fetch_row(static_cast<const T *>(f.w) + j * f.w_stride + i, f.decay != 0.f && j < f.rows_b ? f.rows_a - i : 0, false);
+        } else {
+            Raw<float> old{};
+            if (TO_X && j < f.rows_b && i < padded(f.rows_a)) old = fetch_pairs(f.old_by_j, j, i);
+            return old;
+        }
+    };
     // Eight results of a j, i and the seven behind it: what becomes of them, and there they are for the other way of writing them.
-    const auto finish = [&](int64_t j, int64_t i, float (&v)[8]) {
+    const auto finish = [&](int64_t j, int64_t i, float (&v)[8], const auto &before) {
         if constexpr (MODE == GRAM || MODE == NEXT) {
 #pragma unroll
             for (int x = 0; x < 8; ++x) v[x] *= MODE == GRAM ? 1.f / ONE : 1.f / ONE_OF_B;
-            if constexpr (MODE == NEXT && Tile::FORM == HIGH) {
-                float old[8] = {};
-                if (j < f.rows_b && i < padded(f.rows_a)) get_pairs(f.old_by_j, j, i, old);
+            if constexpr (TO_X) {
+                float old[8];
+                unpack_pairs(before, old);
 #pragma unroll
                 for (int x = 0; x < 8; ++x) v[x] = __builtin_fmaf(NS_A, old[x], v[x]);
             }
@@ -245,7 +259,7 @@ template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_
             for (int x = 0; x < 8; ++x) v[x] *= f.scale * (1.f / ONE / ONE_OF_B);
             if (f.decay != 0.f) {
                 float old[8];
-                unpack(load_row(to, f.rows_a - i, false), old);
+                unpack(before, old);
 #pragma unroll
                 for (int x = 0; x < 8; ++x) v[x] = __builtin_fmaf(f.decay, old[x], v[x]);
             }
@@ -285,7 +299,7 @@ template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_
 #pragma unroll
                 for (int x = 0; x < 8; ++x) v[x] += t[x];
             }
-            finish(b0 + j, a0 + i, v);
+            finish(b0 + j, a0 + i, v, before(b0 + j, a0 + i));
             if (both) {
                 const Raw<float> r = pack<float>(v);
                 U4 *const at = reinterpret_cast<U4 *>(sums + j * PITCH + i);
@@ -310,19 +324,28 @@ template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_
             __builtin_amdgcn_wave_barrier();
         };
         float *const mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
-        const int64_t i_at = a0 + wm * (Tile::BM / Tile::WM);
+        const int64_t i_at = a0 + wm * (Tile::BM / Tile::WM), j_first = b0 + wn * (Tile::BN / Tile::WN);
+        // What the next 32 j's results are added to is asked for while the last ones' are written.
+        constexpr int ITEMS = OCTETS / 2, TOGETHER = TO_X || TO_W ? ITEMS : 2;
+        decltype(before(0, 0)) old[TO_X || TO_W ? ITEMS : 1];
+        const auto ask = [&](int n) {
+            if constexpr (TO_X || TO_W)
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) old[k] = before(j_first + n * 32 + (lane + 64 * k) / OCTETS, i_at + (lane + 64 * k) % OCTETS * 8);
+        };
+        ask(0);
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
-            const int64_t j_at = b0 + wn * (Tile::BN / Tile::WN) + n * 32;
+            const int64_t j_at = j_first + n * 32;
             lay(mine, n);
             together();
-#pragma unroll 2
-            for (int item = lane; item < 32 * OCTETS; item += 64) {
-                const int k = item / OCTETS, octet = item % OCTETS;
+#pragma unroll TOGETHER
+            for (int which = 0; which < ITEMS; ++which) {
+                const int item = lane + 64 * which, k = item / OCTETS, octet = item % OCTETS;
                 U4 *const at = reinterpret_cast<U4 *>(mine + k * PITCH + octet * 8);
                 float v[8];
                 unpack(Raw<float>{{at[0], at[1]}}, v);
-                finish(j_at + k, i_at + octet * 8, v);
+                finish(j_at + k, i_at + octet * 8, v, old[TO_X || TO_W ? which : 0]);
                 if (both) {
                     const Raw<float> r = pack<float>(v);
                     at[0] = r.w[0];
@@ -330,6 +353,7 @@ template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_
                 }
             }
             together();
+            if (n + 1 < NI) ask(n + 1);
             if constexpr (MODE != LAST && MODE != SHARE) {
                 if (both) {
 #pragma unroll 2
@@ -410,9 +434,9 @@ struct Choice {
     int split, per;
 };
 constexpr int SPLIT_MAX = 16;
-// us: of a slice on a full chip, from pairs (32 elements) and from the h alone (64, of which a compute unit fetches as many lines), and what a workgroup takes beside its
-// slices.  Measured on 1600 x 6400: X = B X from pairs 129, 115, 104, 115, 135 us by tile, from the h alone (and written as w) 64, 61, 65, 77, 109; X X^T
-// from pairs (with the join) 80, -, -, 68, 82, from the h alone 51, -, -, 48, 87; A A 45, -, -, 35, 30 and 34, -, -, 34, 24.
+// us: of a slice on a full chip, from pairs (32 elements) and from the h alone (64), and what a workgroup takes beside its slices.  Measured on 1600 x 6400: X = B X
+// from pairs 129, 115, 104, 115, 135 us by tile, from the h alone 83, 72, 74, 74, 75, written as w 59, 50, 51, 57, 68; X X^T from pairs (with the join) 80, -, -,
+// 68, 82, from the h alone 48, -, -, 38, 46; A A 45, -, -, 35, 30 and 28, -, -, 26, 22.
 constexpr double STEP[2][SHAPES] = {{2.3, 2.05, 1.85, 1.45, 0.72}, {2.0, 1.95, 2.1, 1.5, 1.1}}, BESIDE[SHAPES] = {14., 12., 11., 8., 5.};
 constexpr double DEEP_STEP = 0.17;  // of Deep64
 enum Writes { HALF, X, X_AS_IT_LIES, W };  // a symmetric matrix; X, either operand first or the first one; w
