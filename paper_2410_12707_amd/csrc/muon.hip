@@ -312,7 +312,7 @@ template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_
         __syncthreads();
 #pragma unroll 2
         for (int item = threadIdx.x; item < Tile::BM * (Tile::BN / 8); item += Tile::NT) {
-            const int i = item % Tile::BM, eight = item / Tile::BM * 8;
+            const int i = item / 4 % Tile::BM, eight = (item / 4 / Tile::BM * 4 + item % 4) * 8;
             float v[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) v[x] = sums[(eight + x) * PITCH + i];
@@ -357,8 +357,8 @@ template <Mode MODE, typename T, typename Tile, int PER_CU> __global__ __launch_
             if constexpr (MODE != LAST && MODE != SHARE) {
                 if (both) {
 #pragma unroll 2
-                    for (int item = lane; item < MI * 128; item += 64) {  // an octet of j for an i
-                        const int i = item % (MI * 32), eight = item / (MI * 32) * 8;
+                    for (int item = lane; item < MI * 128; item += 64) {  // an octet of j for an i; four lanes write 64 bytes of h, then of l
+                        const int i = item / 4, eight = item % 4 * 8;
                         float v[8];
 #pragma unroll
                         for (int x = 0; x < 8; ++x) v[x] = mine[(eight + x) * PITCH + i];
@@ -437,7 +437,7 @@ constexpr int SPLIT_MAX = 16;
 // us: of a slice on a full chip, from pairs (32 elements) and from the h alone (64), and what a workgroup takes beside its slices.  Measured on 1600 x 6400: X = B X
 // from pairs 129, 115, 104, 115, 135 us by tile, from the h alone 83, 72, 74, 74, 75, written as w 59, 50, 51, 57, 68; X X^T from pairs (with the join) 80, -, -,
 // 68, 82, from the h alone 48, -, -, 38, 46; A A 45, -, -, 35, 30 and 28, -, -, 26, 22.
-constexpr double STEP[2][SHAPES] = {{2.3, 2.05, 1.85, 1.45, 0.72}, {2.0, 1.95, 2.1, 1.5, 1.1}}, BESIDE[SHAPES] = {14., 12., 11., 8., 5.};
+constexpr double STEP[2][SHAPES] = {{2.3, 2.05, 1.85, 1.45, 0.76}, {2.0, 1.95, 2.1, 1.5, 1.1}}, BESIDE[SHAPES] = {14., 12., 11., 8., 5.};
 constexpr double DEEP_STEP = 0.17;  // of Deep64
 enum Writes { HALF, X, X_AS_IT_LIES, W };  // a symmetric matrix; X, either operand first or the first one; w
 Choice choice_of(int64_t rows_a, int64_t rows_b, int64_t sum, Writes writes, bool high) {

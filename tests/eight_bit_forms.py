@@ -20,7 +20,7 @@ PRODUCTS = [
 UPDATES = [
     (0, (64, 64), True, False, (257, 300)), (0, (64, 64), True, True, (70, 3001)), (0, (64, 64), False, False, (1927, 1983)), (0, (64, 64), False, True, (1419, 1421)),
     (0, (128, 128), False, False, (3221, 3306)), (0, (128, 128), False, True, (1765, 1781)), (0, (256, 256), False, False, (4938, 4891)), (0, (256, 256), False, True, (3745, 1947)),
-    (1, (64, 64), True, False, (257, 300)), (1, (64, 64), False, False, (1794, 1898)), (1, (64, 64), False, True, (1419, 1421)), (1, (128, 128), False, False, (3221, 3306)),
+    (1, (64, 64), True, False, (257, 300)), (1, (64, 64), False, False, (1927, 1983)), (1, (64, 64), False, True, (1419, 1421)), (1, (128, 128), False, False, (3221, 3306)),
     (1, (128, 128), False, True, (1765, 1781)), (1, (256, 256), False, False, (4938, 4891)), (1, (256, 256), False, True, (2978, 2993)),
     (2, (64, 64), True, False, (257, 300)), (2, (64, 64), False, False, (1419, 1421)), (2, (128, 128), False, False, (65, 36734)), (2, (160, 256), False, False, (129, 39956)),
     (2, (192, 256), False, False, (161, 43484)), (2, (256, 256), False, False, (193, 49487)),
