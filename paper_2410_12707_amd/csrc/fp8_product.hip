@@ -1,9 +1,14 @@
 // The product of two matrices in 8-bit floating point, y = x W^T + bias + add.
 //
 // The scales are powers of two, a byte for 128 of a row: the matrix instruction applies them as it goes, or the conversion to bf16 where results are fp32
-// (row_tiles.h says why); products are exact and sums are fp32, one chain over the sum's axis per share of it.  The weights are the instruction's first operand, so that a lane's results are neighbours in a row of y.  Three forms: tiles of
-// row_tiles.h, each workgroup one; the same with the sum's axis shared out where tiles are few, partial sums to the workspace and k_fp8_join behind; and for a few
-// tokens k_fp8_few, which reads the weights once and straight into registers.
+// (row_tiles.h says why); products are exact and sums are fp32, one chain over the sum's axis per share of it.  The weights are the instruction's first operand, so that
+// a lane's results are neighbours in a row of y.  Three forms: tiles of row_tiles.h, each workgroup one; the same with the sum's axis shared out where tiles are few,
+// partial sums to the workspace and k_fp8_join behind; and for a few tokens k_fp8_few, which reads the weights once and straight into registers.
+//
+// Measured, us, 16-bit results and fp32 ones: one token 1600 -> 6400 4.1, 5.1; 512 tokens 768 -> 768 5.8, 6.8; 2048 x 2048 x 2048 16.5, 24.8; 4096 x 4096 x 4096 56, 112 (2.5
+// and 1.2 PFLOP/s); 16384 tokens 1600 -> 6400 185, 311 (1.8 and 1.1), where a library's product with one scale for each matrix takes 200.  Large products are bound by the
+// matrix unit's power (of zeros 4096 x 4096 x 8192 takes 87, of noise 107), small ones by the launch and the latency of the first slices, a few tokens' by the
+// weights' bytes.
 #include <hip/hip_runtime.h>
 
 #ifdef ADATOPK_MEASURE_BUILD

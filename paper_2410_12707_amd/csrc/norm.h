@@ -155,7 +155,7 @@ template <bool CENTRED, typename T, bool KEEP> __device__ __forceinline__ void c
 // registers of keeping them as floats, which the next row's operands take.  KEEP: h comes from the 8-bit rows.
 // COLUMNS: the weight's gradient is not added up along with the rows, but, where it is asked for, by workgroups before those of the rows.
 // 16384 x 1600 bf16 from 8-bit rows with the residual's gradient: 41.5 us and 4 of the join, 4.1 TB/s; from x without it 39 us, 4.0 TB/s; 32768 x 768 fp32
-// 54 us, 5.6 TB/s; 1000 x 1601 fp16 7.7 us.  What holds it below the forward pass is registers: the weight's gradient takes 16 for each octet, so a compute
+// 54 us, 5.6 TB/s; 1000 x 1601 fp16 7.7 us.  Without the centre 16384 x 1600 so 34 us and 4.6, 5.4 TB/s; 1000 x 1601 fp16 7.6.  What holds it below the forward pass is registers: the weight's gradient takes 16 for each octet, so a compute
 // unit has half the loads on their way.  Two rows ahead instead of one cost more in moves or wavefronts than they hid (57 to 67 us where this took 52).
 // 1024 x 20000 bf16: 87 us, 38 without the weight's gradient, whose columns are read a second time in pieces of 64 bytes.
 template <bool CENTRED, typename T, int L, int S, bool KEEP, bool COLUMNS> __global__ __launch_bounds__(threads_of(L)) void k_norm_backward(Backward f) {
