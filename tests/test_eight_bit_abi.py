@@ -141,6 +141,21 @@ def test_the_binding_refuses(monkeypatch):
         B.adatopk_fp8_store(Fake(torch.zeros(4, 64, dtype=torch.float64)), Fake(torch.zeros(4096, dtype=torch.uint8)))
 
 
+def test_what_is_not_plain_is_left_to_python():
+    m, a = B._load_marshal(), B.load_library().address
+    x, u8, w = torch.zeros(4, 64), torch.zeros(1024, dtype=torch.uint8), torch.zeros(4, 64)  # not in device memory
+    for call in (lambda: m.fp8_store(a.fp8_store, x, u8), lambda: m.fp8_load(a.fp8_load, u8, x), lambda: m.fp8_store_weight(a.fp8_store_weight, w, u8, None),
+                 lambda: m.fp8_product(a.fp8_product, u8, u8, 64, x, u8, None, None), lambda: m.rmsnorm_forward(a.rmsnorm_forward, x, None, 1e-5, x, None, None, None, None, None),
+                 lambda: m.rmsnorm_backward(a.rmsnorm_backward, x, x, None, x[:, 0], None, x, None, None, None, False),
+                 lambda: m.muon_update(a.muon_update, w, None, 0.0, False, w, 1.0, 0.0, u8, 5, 1e-7)):
+        assert call() is None
+    for call, count in ((m.fp8_store, 3), (m.fp8_load, 3), (m.fp8_store_weight, 4), (m.fp8_product, 8), (m.rmsnorm_forward, 10), (m.rmsnorm_backward, 11), (m.muon_update, 11)):
+        for wrong in ((None,) * count, ("x", 1, 2.0, [], {}, (), 0, None, "y", 3, b"")[:count]):
+            assert call(*wrong) is None
+        with pytest.raises(TypeError):
+            call(*(None,) * (count + 1))
+
+
 def test_sizes_for_every_form_take_the_form_they_are_meant_for():
     for dtype, form, size in forms.PRODUCTS:
         side, along, split, quarters = B.measure_fp8_product_cut(*size, dtype)
