@@ -44,6 +44,7 @@ struct Pairs {
     uint8_t *at;
     int64_t pitch;
     int run;
+    bool halves;  // only h are written: nobody reads the l
 };
 constexpr int run_for(bool high) { return high ? 6 : 5; }
 constexpr int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
@@ -64,7 +65,7 @@ __device__ __forceinline__ void put_pairs(const Pairs &p, int64_t row, int64_t c
     }
     uint8_t *const to = octet_of(p, row, col);
     *reinterpret_cast<U4 *>(to) = pack<F16>(h).w[0];
-    *reinterpret_cast<U4 *>(to + (2 << p.run)) = pack<F16>(l).w[0];
+    if (!p.halves) *reinterpret_cast<U4 *>(to + (2 << p.run)) = pack<F16>(l).w[0];
 }
 __device__ __forceinline__ Raw<float> fetch_pairs(const Pairs &p, int64_t row, int64_t col) {
     const uint8_t *const from = octet_of(p, row, col);
@@ -587,10 +588,23 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
     const bool coarser = dt != ADATOPK_F32 && less >= COARSE_FROM, coarse_end = coarser && dt == ADATOPK_BF16;
     const int fine = !coarser ? steps : dt == ADATOPK_F16 ? 3 : 2;
     const auto high_at = [&](int step) { return steps - step > fine || (coarse_end && step + 1 == steps); };
-    const auto pairs = [&](size_t where, int64_t of) { return Pairs{base + where, padded(of) * 4, run_for(high_at(0))}; };
+    const auto pairs = [&](size_t where, int64_t of) { return Pairs{base + where, padded(of) * 4, run_for(high_at(0)), false}; };
     Pairs x = pairs(at.x, more), gram = pairs(at.gram, less), poly = pairs(at.poly, less);
     Pairs xt = pairs(at.xt[0], less), xt_next = pairs(at.xt[1], less);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+
+    const Choice next = choice_of(less, more, less, X, false), next_coarse = choice_of(less, more, less, X, true);
+    // (X's runs change: turned, it would be read and written in place in two orders)
+    const Choice next_changing = choice_of(less, more, less, X_AS_IT_LIES, true);
+    const Choice last = choice_of(cols, rows, less, W, coarse_end);
+    // X as `step` reads it: its l by products from pairs, and one of the two X by a coarse step, which adds to it.
+    const auto coarse_of = [&](int step) -> const Choice & { return high_at(step + 1) ? next_coarse : next_changing; };
+    const auto as_read_at = [&](int step, Pairs &rows_first, Pairs &turned) {
+        rows_first.run = turned.run = run_for(high_at(step));
+        rows_first.halves = high_at(step) && (step + 1 == steps || !coarse_of(step).turned);
+        turned.halves = high_at(step) && (step + 1 == steps || coarse_of(step).turned);
+    };
+    as_read_at(0, x, xt);
 
     const int64_t per_row = (cols + 7) / 8, octets = rows * per_row;
     const unsigned mix = static_cast<unsigned>((octets + 255) / 256 < MIX_GROUPS ? (octets + 255) / 256 : MIX_GROUPS);
@@ -604,13 +618,10 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
     });
 
     const int along = static_cast<int>(padded(more) / 32), side = static_cast<int>(padded(less) / 32);
-    const Choice next = choice_of(less, more, less, X, false), next_coarse = choice_of(less, more, less, X, true);
-    // (X's runs change: turned, it would be read and written in place in two orders)
-    const Choice next_changing = choice_of(less, more, less, X_AS_IT_LIES, true);
-    const Choice last = choice_of(cols, rows, less, W, coarse_end);
     for (int step = 0; step < steps; ++step) {
         const bool high = high_at(step);
         x.run = xt.run = gram.run = poly.run = run_for(high);
+        poly.halves = high;
         Product p{};
         p.partial = reinterpret_cast<float *>(base + at.shares);
         p.a = p.b = x;
@@ -630,11 +641,11 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
             p.rows_b = more;
             p.by_j = xt_next;
             p.by_i = x;
-            p.by_j.run = p.by_i.run = run_for(high_at(step + 1));
+            as_read_at(step + 1, p.by_i, p.by_j);
             p.old_by_j = xt;
             p.old_by_i = x;
             if (coarse)
-                launch_product<NEXT, float, HIGH>(p, high_at(step + 1) ? next_coarse : next_changing, st);
+                launch_product<NEXT, float, HIGH>(p, coarse_of(step), st);
             else
                 launch_product<NEXT, float, PAIRS>(p, next, st);
             const Pairs t = xt;
