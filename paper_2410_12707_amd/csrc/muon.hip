@@ -17,9 +17,9 @@
 // fp16, whose own rounding is 2e-4 in the 2-norm, the second where it is bf16, whose rounding is 1.7e-3.  With fewer than 256 rows less is levelled (16 x 100:
 // 1.4e-3 and 4.3e-3 at the worst of eight) and products are not what takes the time: there all steps take the full 22 bits.
 //
-// Measured, five steps, us, of bf16, fp16 and fp32 weights: 768 x 768 143, 157, 170; 1024 x 4096 267, 313, 367; 1600 x 6400 640, 798, 932; 4096 x 4096 2275, 3095, 3930.  Of the
+// Measured, five steps, us, of bf16, fp16 and fp32 weights: 768 x 768 141, 153, 167; 1024 x 4096 257, 305, 358; 1600 x 6400 603, 758, 898; 4096 x 4096 2163, 3002, 3837.  Of the
 // largest the matrix unit's share at a library product's rate is 1.5, 2.4 and 3.2 ms.  What bounds the rest: a B X writes X twice at the end of its one round of tiles, with nothing to
-// cover it (at 1600 x 6400 some 25 us of 65 from halves, of 92 from pairs); small matrices' products are 10 us each whatever they compute, start, six slices' latency and
+// cover it (at 1600 x 6400 some 20 us of 60 from halves); small matrices' products are 10 us each whatever they compute, start, six slices' latency and
 // end, and each needs the one before.
 #include <hip/hip_runtime.h>
 
