@@ -420,14 +420,22 @@ adatopk_status adatopk_rmsnorm_backward(const void *dy, int64_t dy_stride, const
  *   steps        1 ... 64; five take singular values from 0.01 ... 1 of |u| to 0.7 ... 1.2
  *   w            rows x cols values of dt
  *   workspace    device, 256-byte aligned, at least adatopk_muon_update_workspace_bytes(rows, cols)
- * Everything between the steps carries 22 bits, sums are fp32 and |u| a 64-bit sum; w is rounded once: fp32's X is 4e-7 to 8e-6 off (2-norm, relative), like one of
- * fp32 throughout.  Where w is of 16 bits and its shorter side 256 or more, products of some steps take 11 bits: X is 6e-6 to 9e-5 off in fp16, 4e-4 to 1e-3 in bf16, less
- * than w's own rounding there.  The order of all sums is fixed: equal calls give equal bits.  A NaN or an infinity in u makes all of X NaN.
+ * Everything between the steps carries 22 bits, sums are fp32 and |u| a 64-bit sum; w is rounded once, whatever its type.  So X is about as far off as with fp32
+ * throughout: 2e-7 to 7e-6 (2-norm, relative; 256 to 1600 rows of noise, few rows, low rank with noise, three to twelve steps).  In either, what roundings leave in
+ * directions in which u has next to nothing grows 3.4-fold in each step until it comes to 0.7: of rank 4 X is 4e-5 to 1.3e-4 off after five steps and up to 4e-3 after
+ * eight.  The order of all sums is fixed: equal calls give equal bits.  A NaN or an infinity in u makes all of X NaN.
  * rows, cols <= 65536, rows * cols < 2^31. */
 size_t adatopk_muon_update_workspace_bytes(int64_t rows, int64_t cols);
 adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatopk_dtype grad_dt, float *momentum, float mu, int32_t nesterov, int64_t rows,
                                    int64_t cols, int32_t steps, float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay,
                                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The same in fewer bits and less time where w is of 16 bits and its shorter side 256 or more (elsewhere the two calls are one): products of all steps but the last
+ * three (bf16: two), and bf16's last one, take 11 bits.  How far X is off depends on the gradient, least of noise, most where a few rows are nearly all there is: after five
+ * steps 5e-6 to 3e-3 in fp16, 5e-4 to 4e-3 in bf16, after twelve up to 1e-2.  w's own rounding is 2e-4 and 1.7e-3. */
+adatopk_status adatopk_muon_update_coarse(const void *grad, int64_t grad_stride, adatopk_dtype grad_dt, float *momentum, float mu, int32_t nesterov, int64_t rows,
+                                          int64_t cols, int32_t steps, float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay,
+                                          void *workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -192,6 +192,8 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.adatopk_muon_update_workspace_bytes.restype = sz
     lib.adatopk_muon_update.argtypes = [p, i64, i32, p, f32, i32, i64, i64, i32, f32, p, i64, i32, f32, f32, p, sz, p]
     lib.adatopk_muon_update.restype = i32
+    lib.adatopk_muon_update_coarse.argtypes = lib.adatopk_muon_update.argtypes
+    lib.adatopk_muon_update_coarse.restype = i32
     lib.address = _Addresses(lib)
     return lib
 
@@ -203,7 +205,7 @@ class _Addresses:
         for name in ("compress", "decompress", "decompress_sorted", "decompress_accumulate", "decompress_segmented", "compress_wire",
                      "compress_wire_segmented", "decompress_wire", "compress_segmented", "act8_store", "act8_load", "gelu_forward", "gelu_backward",
                      "layernorm_forward", "layernorm_backward", "weight_grad", "fp8_store", "fp8_load", "fp8_store_weight", "fp8_product", "rmsnorm_forward",
-                     "rmsnorm_backward", "muon_update"):
+                     "rmsnorm_backward", "muon_update", "muon_update_coarse"):
             setattr(self, name, ctypes.cast(getattr(lib, "adatopk_" + name), ctypes.c_void_p).value)
 
 
@@ -837,20 +839,22 @@ def adatopk_muon_update_workspace_bytes(rows: int, cols: int) -> int:
 
 
 def adatopk_muon_update(grad: torch.Tensor, momentum: Optional[torch.Tensor], mu: float, nesterov: bool, w: torch.Tensor, scale: float, decay: float,
-                        workspace: torch.Tensor, steps: int = 5, eps: float = 1e-7) -> None:
-    """w = decay * w + scale * (the orthogonalised gradient, or momentum, which takes its step first)."""
+                        workspace: torch.Tensor, steps: int = 5, eps: float = 1e-7, coarse: bool = False) -> None:
+    """w = decay * w + scale * (the orthogonalised gradient, or momentum, which takes its step first); coarse: 16-bit weights with products of 11 bits in some steps."""
     lib = load_library()
     m = _marshal or _load_marshal()
-    if m and _done(m.muon_update(lib.address.muon_update, grad, momentum, mu, nesterov, w, scale, decay, workspace, steps, eps), "adatopk_muon_update"):
+    where = "adatopk_muon_update_coarse" if coarse else "adatopk_muon_update"
+    if m and _done(m.muon_update(lib.address.muon_update_coarse if coarse else lib.address.muon_update, grad, momentum, mu, nesterov, w, scale, decay, workspace, steps, eps),
+                   where):
         return
     address, stride, rows, cols = _matrix(w, "w")
     grad_address, grad_stride, grad_rows, grad_cols = _matrix(grad, "grad")
     if (grad_rows, grad_cols) != (rows, cols):
         raise ValueError("grad must have %d rows of %d" % (rows, cols))
-    _check(lib.adatopk_muon_update(
+    _check((lib.adatopk_muon_update_coarse if coarse else lib.adatopk_muon_update)(
         grad_address, grad_stride, _dtype_code(grad.dtype), _floats(momentum, rows * cols, "momentum"), float(mu), 1 if nesterov else 0, rows, cols, int(steps),
         float(eps), address, stride, _dtype_code(w.dtype), float(scale), float(decay), _dev(workspace), workspace.numel() * workspace.element_size(), _stream()),
-        "adatopk_muon_update")
+        where)
 
 
 # ------------------------------------------------------------------ measurement hooks (measuring build only)

@@ -7,20 +7,20 @@
 // symmetric, and X from B and X transposed, so each step writes X both ways; of A and B half the tiles are computed and written twice.
 //
 // Small singular values grow 3.4-fold in each step, and so does what a rounding of X leaves in their directions: with X in bf16 the result is some 2 to 7 % off, in
-// one fp16 1e-3 to 6e-3, in two fp16 4e-7 to 8e-6, like fp32 (512 to 1000 rows, of noise and of low rank with noise; 2-norm of the error, relative).  So
+// one fp16 1e-3 to 6e-3, in two fp16 2e-7 to 7e-6, like fp32 (256 to 1600 rows, of noise, of few rows and of low rank with noise; 2-norm of the error, relative).  So
 // everything between the steps is two fp16, h + l, times 2^14 (A and X stay within 1.5, X's singular values within 1.21: nothing overflows, and l keeps its
 // bits down to 2^-17) or, for B, whose diagonal reaches 3.45, 2^13.  Products are three of the matrix instruction's, sums fp32; |u| is a 64-bit sum.
 //
-// With B X = a X + (b A + c A A) X only the first term matters where singular values are small: a step whose a X is added in the full 22 bits and whose products
-// are of the h alone leaves errors of some 2^-12 in directions that are large, and the steps behind it level most of them.  With all but the last three steps so,
-// the result is 6e-6 to 9e-5 off; with all but the last two, and the last one's products of the h alone, 4e-4 to 1e-3.  The first is taken where w is
-// fp16, whose own rounding is 2e-4 in the 2-norm, the second where it is bf16, whose rounding is 1.7e-3.  With fewer than 256 rows less is levelled (16 x 100:
-// 1.4e-3 and 4.3e-3 at the worst of eight) and products are not what takes the time: there all steps take the full 22 bits.
+// Coarse steps, where the caller asks for them and w has 16 bits.  With B X = a X + (b A + c A A) X only the first term matters where singular values are small: a step
+// whose a X is added in the full 22 bits and whose products are of the h alone leaves errors of some 2^-12 in directions that are large.  How much of them the steps
+// behind it level is the gradient's affair: five steps of which all but the last three are coarse (fp16) are 5e-6 off on noise of 1600 rows, but 3e-3 where five rows are
+// all there is; all but the last two, and the last one's products of the h alone (bf16), 5e-4 to 4e-3.  That is more than w's own rounding (2e-4 and 1.7e-3
+// in the 2-norm), so nobody gets it unasked.  With fewer than 256 rows less is levelled and products are not what takes the time: there all steps take the full 22 bits.
 //
-// Measured, five steps, us, of bf16, fp16 and fp32 weights: 768 x 768 141, 153, 167; 1024 x 4096 257, 305, 358; 1600 x 6400 603, 758, 898; 4096 x 4096 2163, 3002, 3837.  Of the
-// largest the matrix unit's share at a library product's rate is 1.5, 2.4 and 3.2 ms.  What bounds the rest: a B X writes X twice at the end of its one round of tiles, with nothing to
-// cover it (at 1600 x 6400 some 20 us of 60 from halves); small matrices' products are 10 us each whatever they compute, start, six slices' latency and
-// end, and each needs the one before.
+// Measured, five steps, us, and with coarse steps for bf16 and fp16 weights: 768 x 768 168 (140, 155); 1024 x 4096 372 (258, 317); 1600 x 6400 921 (613, 781); 4096 x 4096 3885
+// (2200, 3057).  Of the largest the matrix unit's share at a library product's rate is 3.2 ms (1.5, 2.4).  What bounds the rest: a B X writes X twice at the end of its one
+// round of tiles, with nothing to cover it; small matrices' products are 10 us each whatever they compute, start, six slices' latency and end, and each needs the
+// one before.
 #include <hip/hip_runtime.h>
 
 #ifdef ADATOPK_MEASURE_BUILD
@@ -563,18 +563,10 @@ Workspace workspace_of(int64_t less, int64_t more) {
     return w;
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t adatopk_muon_update_workspace_bytes(int64_t rows, int64_t cols) {
-    if (!update_ok(rows, cols) || rows == 0 || cols == 0) return 0;
-    return workspace_of(rows < cols ? rows : cols, rows < cols ? cols : rows).bytes;
-}
-
-adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatopk_dtype grad_dt, float *momentum, float mu, int32_t nesterov, int64_t rows,
-                                   int64_t cols, int32_t steps, float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay,
-                                   void *workspace, size_t workspace_bytes, void *hip_stream) {
+// `coarse_too`: products of some steps in 11 bits where w has 16.
+adatopk_status update(const void *grad, int64_t grad_stride, adatopk_dtype grad_dt, float *momentum, float mu, int32_t nesterov, int64_t rows, int64_t cols, int32_t steps,
+                      float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay, void *workspace, size_t workspace_bytes, void *hip_stream,
+                      bool coarse_too) {
     if (!dtype_ok(grad_dt) || !dtype_ok(dt) || !update_ok(rows, cols) || steps < 1 || steps > MAX_STEPS || !(eps >= 0.f)) return ADATOPK_EINVAL;
     if (rows == 0 || cols == 0) return ADATOPK_OK;
     if (!matrix_ok(grad, grad_stride, rows, cols, grad_dt) || !matrix_ok(w, w_stride, rows, cols, dt) || !pointer_ok_or_null(momentum, 4) || !pointer_ok(workspace, 256))
@@ -584,8 +576,8 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
     const Workspace at = workspace_of(less, more);
     if (workspace_bytes < at.bytes) return ADATOPK_EWORKSPACE;
     uint8_t *const base = static_cast<uint8_t *>(workspace);
-    // Where w is of 16 bits: products of 11 bits in all steps but the last ones, and in bf16's last.
-    const bool coarser = dt != ADATOPK_F32 && less >= COARSE_FROM, coarse_end = coarser && dt == ADATOPK_BF16;
+    // Where the caller asks for it and w is of 16 bits: products of 11 bits in all steps but the last ones, and in bf16's last.
+    const bool coarser = coarse_too && dt != ADATOPK_F32 && less >= COARSE_FROM, coarse_end = coarser && dt == ADATOPK_BF16;
     const int fine = !coarser ? steps : dt == ADATOPK_F16 ? 3 : 2;
     const auto high_at = [&](int step) { return steps - step > fine || (coarse_end && step + 1 == steps); };
     const auto pairs = [&](size_t where, int64_t of) { return Pairs{base + where, padded(of) * 4, run_for(high_at(0)), false}; };
@@ -670,6 +662,27 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
         }
     }
     return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t adatopk_muon_update_workspace_bytes(int64_t rows, int64_t cols) {
+    if (!update_ok(rows, cols) || rows == 0 || cols == 0) return 0;
+    return workspace_of(rows < cols ? rows : cols, rows < cols ? cols : rows).bytes;
+}
+
+adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatopk_dtype grad_dt, float *momentum, float mu, int32_t nesterov, int64_t rows,
+                                   int64_t cols, int32_t steps, float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream) {
+    return update(grad, grad_stride, grad_dt, momentum, mu, nesterov, rows, cols, steps, eps, w, w_stride, dt, scale, decay, workspace, workspace_bytes, hip_stream, false);
+}
+
+adatopk_status adatopk_muon_update_coarse(const void *grad, int64_t grad_stride, adatopk_dtype grad_dt, float *momentum, float mu, int32_t nesterov, int64_t rows,
+                                          int64_t cols, int32_t steps, float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay,
+                                          void *workspace, size_t workspace_bytes, void *hip_stream) {
+    return update(grad, grad_stride, grad_dt, momentum, mu, nesterov, rows, cols, steps, eps, w, w_stride, dt, scale, decay, workspace, workspace_bytes, hip_stream, true);
 }
 
 #ifdef ADATOPK_MEASURE_BUILD

@@ -109,9 +109,9 @@ class EightBitStage(FeedForwardStage):
         return dx
 
     def update(self, rate: float = 0.02, decay: float = 0.1, mu: float = 0.95) -> None:
-        """The projections' weights after a step's last micro-batch."""
+        """The projections' weights after a step's last micro-batch.  Coarse: their gradients come out of products in 8 bits, some percent off."""
         for name in self.eight:
-            B.adatopk_muon_update(self.grad[name], self.momentum[name], mu, True, getattr(self, name), -rate, 1.0 - rate * decay, self.workspace)
+            B.adatopk_muon_update(self.grad[name], self.momentum[name], mu, True, getattr(self, name), -rate, 1.0 - rate * decay, self.workspace, coarse=True)
         self.put_away()
 
 
