@@ -430,9 +430,10 @@ adatopk_status adatopk_muon_update(const void *grad, int64_t grad_stride, adatop
                                    int64_t cols, int32_t steps, float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay,
                                    void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* The same in fewer bits and less time where w is of 16 bits and its shorter side 256 or more (elsewhere the two calls are one): products of all steps but the last
- * three (bf16: two), and bf16's last one, take 11 bits.  How far X is off depends on the gradient, least of noise, most where a few rows are nearly all there is: after five
- * steps 5e-6 to 3e-3 in fp16, 5e-4 to 4e-3 in bf16, after twelve up to 1e-2.  w's own rounding is 2e-4 and 1.7e-3. */
+/* The same in fewer bits and less time where w is of 16 bits and its shorter side 256 or more (elsewhere the two calls are one): products of the first two steps (bf16:
+ * three), as far as three (two) others come behind, and bf16's last one take 11 bits.  How far X is off depends on the gradient, least of noise, most where a few rows are
+ * nearly all there is: after five steps 5e-6 to 3e-3 in fp16, 5e-4 to 4e-3 in bf16, of three to twelve at the most 6e-3 and 8e-3 (256 to 1600 rows, and beside what
+ * fp32 is off by).  w's own rounding is 2e-4 and 1.7e-3. */
 adatopk_status adatopk_muon_update_coarse(const void *grad, int64_t grad_stride, adatopk_dtype grad_dt, float *momentum, float mu, int32_t nesterov, int64_t rows,
                                           int64_t cols, int32_t steps, float eps, void *w, int64_t w_stride, adatopk_dtype dt, float scale, float decay,
                                           void *workspace, size_t workspace_bytes, void *hip_stream);

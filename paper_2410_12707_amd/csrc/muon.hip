@@ -12,10 +12,11 @@
 // bits down to 2^-17) or, for B, whose diagonal reaches 3.45, 2^13.  Products are three of the matrix instruction's, sums fp32; |u| is a 64-bit sum.
 //
 // Coarse steps, where the caller asks for them and w has 16 bits.  With B X = a X + (b A + c A A) X only the first term matters where singular values are small: a step
-// whose a X is added in the full 22 bits and whose products are of the h alone leaves errors of some 2^-12 in directions that are large.  How much of them the steps
-// behind it level is the gradient's affair: five steps of which all but the last three are coarse (fp16) are 5e-6 off on noise of 1600 rows, but 3e-3 where five rows are
-// all there is; all but the last two, and the last one's products of the h alone (bf16), 5e-4 to 4e-3.  That is more than w's own rounding (2e-4 and 1.7e-3
-// in the 2-norm), so nobody gets it unasked.  With fewer than 256 rows less is levelled and products are not what takes the time: there all steps take the full 22 bits.
+// whose a X is added in the full 22 bits and whose products are of the h alone leaves errors of some 2^-12 in directions that are large.  So they are the first ones, two
+// for fp16 and three for bf16, as far as three (two) others come behind; counted from the end, the sixth step and those behind it had them where singular values are near 1, and
+// noise was 4e-3 off after eight steps instead of 2e-5.  How much of them the steps behind level is the gradient's affair: five steps are 5e-6 off in fp16 on noise of
+// 1600 rows, but 3e-3 where five rows are all there is; in bf16, whose last product is of the h alone too, 5e-4 to 4e-3.  That is more than w's own rounding (2e-4 and
+// 1.7e-3 in the 2-norm), so nobody gets it unasked.  With fewer than 256 rows less is levelled and products are not what takes the time: there all steps take the full 22 bits.
 //
 // Measured, five steps, us, and with coarse steps for bf16 and fp16 weights: 768 x 768 168 (140, 155); 1024 x 4096 372 (258, 317); 1600 x 6400 921 (613, 781); 4096 x 4096 3885
 // (2200, 3057).  Of the largest the matrix unit's share at a library product's rate is 3.2 ms (1.5, 2.4).  What bounds the rest: a B X writes X twice at the end of its one
@@ -576,10 +577,10 @@ adatopk_status update(const void *grad, int64_t grad_stride, adatopk_dtype grad_
     const Workspace at = workspace_of(less, more);
     if (workspace_bytes < at.bytes) return ADATOPK_EWORKSPACE;
     uint8_t *const base = static_cast<uint8_t *>(workspace);
-    // Where the caller asks for it and w is of 16 bits: products of 11 bits in all steps but the last ones, and in bf16's last.
+    // Where the caller asks for it and w is of 16 bits: products of 11 bits in the first steps, while singular values are small, and in bf16's last.
     const bool coarser = coarse_too && dt != ADATOPK_F32 && less >= COARSE_FROM, coarse_end = coarser && dt == ADATOPK_BF16;
-    const int fine = !coarser ? steps : dt == ADATOPK_F16 ? 3 : 2;
-    const auto high_at = [&](int step) { return steps - step > fine || (coarse_end && step + 1 == steps); };
+    const int first = !coarser ? 0 : dt == ADATOPK_F16 ? 2 : 3, fine = dt == ADATOPK_F16 ? 3 : 2;
+    const auto high_at = [&](int step) { return (step < first && steps - step > fine) || (coarse_end && step + 1 == steps); };
     const auto pairs = [&](size_t where, int64_t of) { return Pairs{base + where, padded(of) * 4, run_for(high_at(0)), false}; };
     Pairs x = pairs(at.x, more), gram = pairs(at.gram, less), poly = pairs(at.poly, less);
     Pairs xt = pairs(at.xt[0], less), xt_next = pairs(at.xt[1], less);

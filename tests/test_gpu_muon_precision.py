@@ -1,4 +1,5 @@
 """How far the orthogonalised update of 16-bit weights is off, apart from the weights' own rounding, over gradients that treat roundings differently."""
+import numpy as np
 import pytest
 import torch
 
@@ -70,3 +71,24 @@ def test_16_bit_weights_get_an_update_of_all_bits(size, kind, steps):
         # what is stored is at most half a step of X and the error itself, rounded to half of its own step (or of the smallest one)
         stored = ref.HALF_ULP[dtype] * (ref.HALF_ULP[dtype] + bound) * 1.01 + ref.SMALLEST[dtype] / 2 * exact.numel() ** 0.5 / float(exact.norm())
         assert remainder(g, exact, dtype, steps) <= bound + stored, dtype
+
+
+@pytest.mark.parametrize("steps", [5, 6, 8, 12])
+@pytest.mark.parametrize("kind", ["noise", "rank 16 and noise"])
+@pytest.mark.parametrize("size", SIZES[1:])
+def test_coarse_steps_are_those_of_small_singular_values(size, kind, steps):
+    g = GRADIENTS[kind](torch.Generator(device="cuda").manual_seed(sum(size) + steps), *size)
+    exact, single = orthogonalised(g.double(), steps), orthogonalised(g, steps).double()
+    s = np.linalg.svd(g.double().cpu().numpy(), compute_uv=False)
+    s /= np.sqrt((s * s).sum())
+    # A product of 11 bits puts in 2^-11 of what its terms b x^3 and c x^5 are (2^-12 from either factor); the two steps of fp16 weights are the first, and like every error theirs
+    # grows by 1.6 in each step behind the fifth.
+    coarse = 0.0
+    for _ in range(2):
+        following = 3.4445 * s - 4.7750 * s ** 3 + 2.0315 * s ** 5
+        coarse += 2.0 ** -11 * np.linalg.norm(4.7750 * s ** 3 + 2.0315 * s ** 5) / np.linalg.norm(following)
+        s = following
+    growth = max(1.0, 1.6 ** (steps - 5))
+    bound = 4 * float((single - exact).norm() / exact.norm()) + (64 * 2.0 ** -22 + coarse) * growth
+    stored = ref.HALF_ULP[F16] * (ref.HALF_ULP[F16] + bound) * 1.01 + ref.SMALLEST[F16] / 2 * exact.numel() ** 0.5 / float(exact.norm())
+    assert remainder(g, exact, F16, steps, coarse=True) <= bound + stored
