@@ -69,11 +69,14 @@ size_t adatopk_measure_workspace_offset(int32_t what, int64_t n_total, int32_t n
  *                out[2]          shares of the sum; more than one are joined by a second kernel
  *                out[3]          1: the tiles behind the last full round are done in quarters
  *   muon_update  eight products, three numbers each (sides of a tile, and what out[2] is above, + 64 where its wavefronts take turns along the sum): X X^T, A A,
- *                B X and the last step's B X, which writes w, from pairs, then from their h alone */
+ *                B X and the last step's B X, which writes w, from pairs, then from their h alone
+ *   muon_update_next   B X of a step that others follow, four numbers each (sides of a tile, 1: its wavefronts take turns along the sum, 1: its operands change
+ *                places): from pairs, from their h alone with another such step behind it, and with one from pairs behind it */
 adatopk_status adatopk_measure_weight_grad_cut(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, int64_t dy_stride, int32_t *out);
 adatopk_status adatopk_measure_layernorm_cut(int64_t rows, int64_t cols, int32_t backward, int32_t *out);
 adatopk_status adatopk_measure_fp8_product_cut(int64_t rows, int64_t n_out, int64_t n_in, adatopk_dtype dt, int32_t *out);
 adatopk_status adatopk_measure_muon_update_cut(int64_t rows, int64_t cols, int32_t *out);
+adatopk_status adatopk_measure_muon_update_next_cut(int64_t rows, int64_t cols, int32_t *out);
 
 /* Plain streaming kernels on `hip_stream`; all pointers are device memory, 16-byte
  * aligned; bytes must be a multiple of 16.

@@ -78,6 +78,8 @@ def load_measure_library() -> ctypes.CDLL:
     lib.adatopk_measure_fp8_product_cut.restype = i32
     lib.adatopk_measure_muon_update_cut.argtypes = [ctypes.c_int64, ctypes.c_int64, p]
     lib.adatopk_measure_muon_update_cut.restype = i32
+    lib.adatopk_measure_muon_update_next_cut.argtypes = [ctypes.c_int64, ctypes.c_int64, p]
+    lib.adatopk_measure_muon_update_next_cut.restype = i32
     lib.adatopk_measure_copy.argtypes = [p, p, sz, p]
     lib.adatopk_measure_copy.restype = i32
     lib.adatopk_measure_read_only.argtypes = [p, sz, p, p]
@@ -910,6 +912,14 @@ def measure_muon_update_cut(rows: int, cols: int):
     out = (ctypes.c_int32 * 24)()
     _check(load_measure_library().adatopk_measure_muon_update_cut(int(rows), int(cols), out), "adatopk_measure_muon_update_cut")
     return tuple(((out[3 * i], out[3 * i + 1]), out[3 * i + 2] >= 64, out[3 * i + 2] % 64) for i in range(8))
+
+
+def measure_muon_update_next_cut(rows: int, cols: int):
+    """((sides of a tile, whether its wavefronts take turns along the sum, whether its operands change places)) of X's next step: from pairs, from the halves with
+    another such step behind it, and with one from pairs behind it."""
+    out = (ctypes.c_int32 * 12)()
+    _check(load_measure_library().adatopk_measure_muon_update_next_cut(int(rows), int(cols), out), "adatopk_measure_muon_update_next_cut")
+    return tuple(((out[4 * i], out[4 * i + 1]), bool(out[4 * i + 2]), bool(out[4 * i + 3])) for i in range(3))
 
 
 def measure_copy(dst: torch.Tensor, src: torch.Tensor) -> None:

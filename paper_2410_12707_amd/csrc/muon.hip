@@ -706,6 +706,20 @@ adatopk_status adatopk_measure_muon_update_cut(int64_t rows, int64_t cols, int32
     }
     return ADATOPK_OK;
 }
+adatopk_status adatopk_measure_muon_update_next_cut(int64_t rows, int64_t cols, int32_t *out) {
+    if (!update_ok(rows, cols) || rows == 0 || cols == 0) return ADATOPK_EINVAL;
+    const int64_t less = rows < cols ? rows : cols, more = rows < cols ? cols : rows;
+    const Choice three[] = {choice_of(less, more, less, X, false), choice_of(less, more, less, X, true), choice_of(less, more, less, X_AS_IT_LIES, true)};
+    for (int k = 0; k < 3; ++k) {
+        const Choice &c = three[k];
+        const int64_t a = ((c.turned ? more : less) + SHAPE_BM[c.shape] - 1) / SHAPE_BM[c.shape], b = ((c.turned ? less : more) + SHAPE_BN[c.shape] - 1) / SHAPE_BN[c.shape];
+        out[4 * k] = SHAPE_BM[c.shape];
+        out[4 * k + 1] = SHAPE_BN[c.shape];
+        out[4 * k + 2] = c.shape == SHAPE_64 && a * b <= 256 ? 1 : 0;
+        out[4 * k + 3] = c.turned ? 1 : 0;
+    }
+    return ADATOPK_OK;
+}
 #endif
 
 }  // extern "C"
