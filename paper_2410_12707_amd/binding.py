@@ -840,6 +840,15 @@ def adatopk_muon_update_workspace_bytes(rows: int, cols: int) -> int:
     return int(load_library().adatopk_muon_update_workspace_bytes(int(rows), int(cols)))
 
 
+def _momentum(t: Optional[torch.Tensor], rows: int, cols: int):
+    if t is None:
+        return None
+    shape = t.shape
+    if t.dtype != torch.float32 or t.numel() != rows * cols or (len(shape) > 1 and shape[-1] != cols):
+        raise ValueError("momentum must be float32 with %d rows of %d" % (rows, cols))
+    return _dev(t)
+
+
 def adatopk_muon_update(grad: torch.Tensor, momentum: Optional[torch.Tensor], mu: float, nesterov: bool, w: torch.Tensor, scale: float, decay: float,
                         workspace: torch.Tensor, steps: int = 5, eps: float = 1e-7, coarse: bool = False) -> None:
     """w = decay * w + scale * (the orthogonalised gradient, or momentum, which takes its step first); coarse: 16-bit weights with products of 11 bits in some steps."""
@@ -854,7 +863,7 @@ def adatopk_muon_update(grad: torch.Tensor, momentum: Optional[torch.Tensor], mu
     if (grad_rows, grad_cols) != (rows, cols):
         raise ValueError("grad must have %d rows of %d" % (rows, cols))
     _check((lib.adatopk_muon_update_coarse if coarse else lib.adatopk_muon_update)(
-        grad_address, grad_stride, _dtype_code(grad.dtype), _floats(momentum, rows * cols, "momentum"), float(mu), 1 if nesterov else 0, rows, cols, int(steps),
+        grad_address, grad_stride, _dtype_code(grad.dtype), _momentum(momentum, rows, cols), float(mu), 1 if nesterov else 0, rows, cols, int(steps),
         float(eps), address, stride, _dtype_code(w.dtype), float(scale), float(decay), _dev(workspace), workspace.numel() * workspace.element_size(), _stream()),
         where)
 

@@ -641,6 +641,10 @@ PyObject *muon_update(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
         c.plain = c.plain && grad.rows == w.rows && grad.cols == w.cols;
         const adatopk_dtype grad_dt = c.dtype(grad.type), dt = c.dtype(w.type);
         float *momentum = floats(c, a[2], c.plain ? w.rows * w.cols : 0);
+        if (c.plain && a[2] != Py_None) {  // in w's rows, or all of them in one
+            const at::Tensor &m = THPVariable_Unpack(a[2]);
+            c.plain = m.dim() < 2 || m.size(m.dim() - 1) == w.cols;
+        }
         const float mu = real(c, a[3]), scale = real(c, a[6]), decay = real(c, a[7]), eps = real(c, a[10]);
         const int nesterov = c.truth(a[4]);
         const Workspace ws(c, a[8]);
