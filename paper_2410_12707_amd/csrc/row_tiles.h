@@ -36,17 +36,21 @@ __device__ __forceinline__ uint64_t lanes_if_less(int a, int b) {
     asm volatile("s_cmp_lt_i32 %1, %2\n\ts_cselect_b64 %0, -1, 0" : "=s"(lanes) : "s"(a), "s"(b) : "scc");
     return lanes;
 }
+// (The compiler has no value of its own in m0 but what it writes there right before a use, and warns that it would not keep one; that these write it is said all the same.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 // From global memory straight into LDS: 16 (4) bytes per lane of `lanes`, from base + offset, to `to` + 16 (4) * lane.  All lanes of the wavefront are active
 // around it.  Not waited for.  (Written out because the compiler waits for all of them before any read from LDS; there is no register in it that could be
 // taken for written too early.)
 __device__ __forceinline__ void copy_16(uint64_t base, uint32_t offset, uint32_t to, uint64_t lanes) {
     asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(offset), "s"(base), "s"(lanes)
-                 : "memory");
+                 : "memory", "m0");
 }
 __device__ __forceinline__ void copy_4(uint64_t base, uint32_t offset, uint32_t to, uint64_t lanes) {
     asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(offset), "s"(base), "s"(lanes)
-                 : "memory");
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void *)p));
 }
