@@ -353,7 +353,7 @@ adatopk_status adatopk_weight_grad(const void *dy, int64_t dy_stride, const void
  * So the error is at most 2^-4 of the element or, below 2^-6 * 2^(S - 127), at most 2^-10 * 2^(S - 127).  S = 255 marks a block with a NaN or an infinity; all
  * its numbers are NaN.  (Within 2^-5 of a type's largest number an element may be read back as an infinity of the type.)  The buffer: rows of numbers, each padded with zeros to a multiple of 128; from the next multiple of 256 bytes on one byte S
  * per block: those of the rows' first blocks, padded (with anything) to a multiple of 256 rows, then those of the second, and so on.  16-byte aligned.
- * The scales are what the matrix instruction takes (E8M0), so a product costs nothing for them. */
+ * The scales are what the matrix instruction takes (E8M0), so a product costs nothing for them.  Rows times columns, columns rounded up to 128, stay below 2^34. */
 
 /* Host-only.  Bytes of the buffer of a rows x cols matrix; 0 for invalid sizes. */
 size_t adatopk_fp8_bytes(int64_t rows, int64_t cols);

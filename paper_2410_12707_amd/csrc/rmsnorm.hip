@@ -149,7 +149,8 @@ extern "C" {
 adatopk_status adatopk_rmsnorm_forward(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight,
                                        adatopk_dtype weight_dt, int64_t rows, int64_t cols, adatopk_dtype dt, float eps, void *sum, int64_t sum_stride, void *y,
                                        int64_t y_stride, float *rstd, void *act8, void *fp8, void *hip_stream) {
-    if (!dtype_ok(dt) || !(weight_dt == dt || weight_dt == ADATOPK_F32) || !shape_ok(rows, cols) || !fp8_shape_ok(rows, cols) || cols > MAX_COLS || !(eps >= 0.f))
+    if (!dtype_ok(dt) || !(weight_dt == dt || weight_dt == ADATOPK_F32) || !shape_ok(rows, cols) || (fp8 != nullptr && !fp8_shape_ok(rows, cols)) || cols > MAX_COLS ||
+        !(eps >= 0.f))
         return ADATOPK_EINVAL;
     if (rows == 0 || cols == 0) return ADATOPK_OK;
     if (!matrix_ok(x, x_stride, rows, cols, dt) || (y != nullptr ? !matrix_ok(y, y_stride, rows, cols, dt) : fp8 == nullptr) || !weights_ok(weight, weight_dt) ||
