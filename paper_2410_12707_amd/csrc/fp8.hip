@@ -136,7 +136,8 @@ adatopk_status adatopk_fp8_store(const void *x, int64_t x_stride, int64_t rows, 
 
 adatopk_status adatopk_fp8_store_weight(const void *w, int64_t w_stride, int64_t rows, int64_t cols, adatopk_dtype dt, void *fp8, void *fp8_transposed,
                                         void *hip_stream) {
-    if (!dtype_ok(dt) || !fp8_shape_ok(rows, cols) || !fp8_shape_ok(cols, rows)) return ADATOPK_EINVAL;
+    if (!dtype_ok(dt) || rows < 0 || cols < 0 || (fp8 != nullptr && !fp8_shape_ok(rows, cols)) || (fp8_transposed != nullptr && !fp8_shape_ok(cols, rows)))
+        return ADATOPK_EINVAL;
     if (rows == 0 || cols == 0) return ADATOPK_OK;
     if (!matrix_ok(w, w_stride, rows, cols, dt) || !pointer_ok_or_null(fp8, 16) || !pointer_ok_or_null(fp8_transposed, 16) ||
         (fp8 == nullptr && fp8_transposed == nullptr))
