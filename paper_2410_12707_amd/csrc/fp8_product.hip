@@ -5,8 +5,8 @@
 // a lane's results are neighbours in a row of y.  Three forms: tiles of row_tiles.h, each workgroup one; the same with the sum's axis shared out where tiles are few,
 // partial sums to the workspace and k_fp8_join behind; and for a few tokens k_fp8_few, which reads the weights once and straight into registers.
 //
-// Measured, us, 16-bit results and fp32 ones: one token 1600 -> 6400 4.1, 5.1; 512 tokens 768 -> 768 5.8, 6.8; 2048 x 2048 x 2048 16.5, 24.8; 4096 x 4096 x 4096 56, 112 (2.5
-// and 1.2 PFLOP/s); 16384 tokens 1600 -> 6400 185, 311 (1.8 and 1.1), where a library's product with one scale for each matrix takes 200.  Large products are bound by the
+// Measured, us, 16-bit results and fp32 ones: one token 1600 -> 6400 4.2 to 4.6, 4.7; 512 tokens 768 -> 768 5.8, 6.8; 2048 x 2048 x 2048 16.5, 24.8; 4096 x 4096 x 4096 56 to 62, 106 (2.2 to 2.5
+// and 1.3 PFLOP/s); 16384 tokens 1600 -> 6400 175 to 188, 310 (1.8 to 1.9 and 1.1), where a library's product with one scale for each matrix takes 200.  Large products are bound by the
 // matrix unit's power (of zeros 4096 x 4096 x 8192 takes 87, of noise 107), small ones by the launch and the latency of the first slices, a few tokens' by the
 // weights' bytes.
 #include <hip/hip_runtime.h>
@@ -295,7 +295,7 @@ struct Cut {
     int whole;  // tiles; the others in quarters
 };
 // us: of a slice of 128 for a workgroup with a few others on the chip and on a full one, and what a workgroup takes beside; by the 8-bit instruction, and as bf16 for fp32
-// results.  Measured at 14 sizes, 65 x 768 x 768 to 16384 x 1600 x 6400: by tile 193, 216, 302, 550 us there, 57, 69, 115, 140 for 4096 x 4096 x 4096, 17, 8.6, 6.0, 6.4
+// results.  Measured at 14 sizes (and ten of 1 to 64 tokens for FEW_ROWS below), 65 x 768 x 768 to 16384 x 1600 x 6400: by tile 193, 216, 302, 550 us there, 57, 69, 115, 140 for 4096 x 4096 x 4096, 17, 8.6, 6.0, 6.4
 // for 1024 x 1024 x 1024, 57, 24, 17, 11 for 128 x 6400 x 1600.
 constexpr double STEP_ALONE[2][TILED] = {{1.0, 0.38, 0.25, 0.125}, {1.95, 0.66, 0.38, 0.2}}, STEP_FULL[2][TILED] = {{1.5, 0.88, 0.69, 0.16}, {3.1, 1.7, 1.1, 0.26}};
 constexpr double BESIDE[2][TILED] = {{8., 6., 4.8, 5.}, {10., 8., 5.5, 5.3}};

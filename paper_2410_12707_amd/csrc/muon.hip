@@ -7,8 +7,8 @@
 // symmetric, and X from B and X transposed, so each step writes X both ways; of A and B half the tiles are computed and written twice.
 //
 // Small singular values grow 3.4-fold in each step, and so does what a rounding of X leaves in their directions: with X in bf16 the result is some 2 to 7 % off, in
-// one fp16 1e-3 to 6e-3, in two fp16 2e-7 to 7e-6, like fp32 (256 to 1600 rows, of noise, of few rows and of low rank with noise; 2-norm of the error, relative).  So
-// everything between the steps is two fp16, h + l, times 2^14 (A and X stay within 1.5, X's singular values within 1.21: nothing overflows, and l keeps its
+// one fp16 1e-3 to 6e-3 (512 to 1000 rows, of noise and of low rank with noise; 2-norm of the error, relative), in two fp16 2e-7 to 7e-6, like fp32 (256 to 1600
+// rows, few rows with all else nothing among them).  So everything between the steps is two fp16, h + l, times 2^14 (A and X stay within 1.5, X's singular values within 1.21: nothing overflows, and l keeps its
 // bits down to 2^-17) or, for B, whose diagonal reaches 3.45, 2^13.  Products are three of the matrix instruction's, sums fp32; |u| is a 64-bit sum.
 //
 // Coarse steps, where the caller asks for them and w has 16 bits.  With B X = a X + (b A + c A A) X only the first term matters where singular values are small: a step
@@ -443,7 +443,8 @@ struct Choice {
 constexpr int SPLIT_MAX = 16;
 // us: of a slice on a full chip, from pairs (32 elements) and from the h alone (64), and what a workgroup takes beside its slices.  Measured on 1600 x 6400: X = B X
 // from pairs 129, 115, 104, 115, 135 us by tile, from the h alone 83, 72, 74, 74, 75, written as w 59, 50, 51, 57, 68; X X^T from pairs (with the join) 80, -, -,
-// 68, 82, from the h alone 48, -, -, 38, 46; A A 45, -, -, 35, 30 and 28, -, -, 26, 22.
+// 68, 82, from the h alone 48, -, -, 38, 46; A A 45, -, -, 35, 30 and 28, -, -, 26, 22.  (64 from pairs .76 for .72 after 1024 x 4096 fp32: 400 us, 367 with tiles of 128.  At other
+// sizes the choice follows from these costs and has not been measured against the others.)
 constexpr double STEP[2][SHAPES] = {{2.3, 2.05, 1.85, 1.45, 0.76}, {2.0, 1.95, 2.1, 1.5, 1.1}}, BESIDE[SHAPES] = {14., 12., 11., 8., 5.};
 constexpr double DEEP_STEP = 0.17;  // of Deep64
 enum Writes { HALF, X, X_AS_IT_LIES, W };  // a symmetric matrix; X, either operand first or the first one; w

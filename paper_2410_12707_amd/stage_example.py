@@ -12,7 +12,9 @@ are under way (Sec. 3.6) each one's activations wait in 8 bits:
 The matrix products between activations and weights are torch's; everything else is this package's.
 
 With --eight-bit the norm is a root-mean-square norm and the projections, forward and backward, run in 8-bit floating point, from what the norm, GELU and the links
-hand over; behind the last micro-batch the weights are updated by their orthogonalised gradients and put into 8 bits again.  Every product is this package's then.
+hand over; behind the last micro-batch the projections' weights are updated by their orthogonalised gradients and put into 8 bits again (the norm's weight and the biases, whose
+gradients are there too, are a caller's to update).  Every product is this package's then.  It shows the calls together and is not faster at these sizes: GELU, its
+backward pass and the links hand over dense rows, which four more launches per micro-batch put into 8 bits.
 """
 from __future__ import annotations
 
