@@ -8,13 +8,14 @@
 //
 // Small singular values grow 3.4-fold in each step, and so does what a rounding of X leaves in their directions: with X in bf16 the result is some 2 to 7 % off, in
 // one fp16 1e-3 to 6e-3 (512 to 1000 rows, of noise and of low rank with noise; 2-norm of the error, relative), in two fp16 2e-7 to 7e-6, like fp32 (256 to 1600
-// rows, few rows with all else nothing among them).  So everything between the steps is two fp16, h + l, times 2^14 (A and X stay within 1.5, X's singular values within 1.21: nothing overflows, and l keeps its
-// bits down to 2^-17) or, for B, whose diagonal reaches 3.45, 2^13.  Products are three of the matrix instruction's, sums fp32; |u| is a 64-bit sum.
+// rows, few rows with all else nothing among them).  So everything between the steps is two fp16, h + l, times 2^14 (A and X stay within 1.5, X's singular values
+// within 1.21: nothing overflows, and l keeps its bits down to 2^-17) or, for B, whose diagonal reaches 3.45, 2^13.  Products are three of the matrix instruction's, sums
+// fp32; |u| is a 64-bit sum.
 //
 // Coarse steps, where the caller asks for them and w has 16 bits.  With B X = a X + (b A + c A A) X only the first term matters where singular values are small: a step
 // whose a X is added in the full 22 bits and whose products are of the h alone leaves errors of some 2^-12 in directions that are large.  So they are the first ones, two
-// for fp16 and three for bf16, as far as three (two) others come behind; counted from the end, the sixth step and those behind it had them where singular values are near 1, and
-// noise was 4e-3 off after eight steps instead of 2e-5.  How much of them the steps behind level is the gradient's affair: five steps are 5e-6 off in fp16 on noise of
+// for fp16 and three for bf16, as far as three (two) others come behind; counted from the end, updates of more than five steps had them where singular values are near 1, and
+// noise was 4e-3 off after eight steps instead of 2e-5 (512 x 1024, fp16).  How much of them the steps behind level is the gradient's affair: five steps are 5e-6 off in fp16 on noise of
 // 1600 rows, but 3e-3 where five rows are all there is; in bf16, whose last product is of the h alone too, 5e-4 to 4e-3.  That is more than w's own rounding (2e-4 and
 // 1.7e-3 in the 2-norm), so nobody gets it unasked.  With fewer than 256 rows less is levelled and products are not what takes the time: there all steps take the full 22 bits.
 //
